@@ -323,6 +323,87 @@ int jot_gemm_bf16(const void* d_A, const void* d_W, const void* d_residual, void
 int jot_gemm_bf16_noalloc(const void* d_A, const void* d_W, const void* d_residual, void* d_C, int M, int N, int K,
                           int32_t* d_status, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Decoding over a paged key-value cache, for callers that put a step together themselves: the projections are
+ * jot_gemm_bf16's, the head jot_lm_head_stats', and between them stand the four calls below.  (The paper does not
+ * describe them: Section 6.2 measures JoT inside a decoder with a cache, and a program that serves many canvases
+ * keeps that cache in pages.)
+ *   - bf16 or fp16 (`dtype`), fp32 inside.  Strides are in elements; the last dimension is contiguous.  Pointers are
+ *     16-byte aligned, strides multiples of 8, head_dim a multiple of 8, else JOT_ERR_ARG / JOT_ERR_SHAPE.
+ *   - A negative position, slot or length marks padding: what belongs to it stays as it was.
+ *   - Slots, page numbers and lengths live on the device and are checked there: what lies outside the pages is never
+ *     read or written (a slot is skipped; a page reads as zeros; a length counts up to the end of the table's row), and
+ *     *d_status (int32, nullable, never reset) becomes JOT_STATUS_BAD_INDEX.
+ *   - Nothing is allocated and nothing synchronises; the calls may be captured into a CUDA graph. */
+enum { JOT_BF16 = 0, JOT_FP16 = 1 };
+enum { JOT_STATUS_BAD_INDEX = 6 };
+
+/* Pages of all layers: element (layer, page, head, offset, d) of k lies at
+ *   k + layer * k_layer_stride + page * k_page_stride + (head * page_size + offset) * head_dim + d,
+ * likewise v.  n_pages * page_size < 2^31.  Two pages never overlap. */
+typedef struct {
+    void *k, *v;
+    int64_t k_layer_stride, v_layer_stride, k_page_stride, v_page_stride;
+    int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim;
+    int32_t dtype;           /* JOT_BF16 or JOT_FP16 */
+} jot_kv_pages;
+
+/* Position rotation: pair i of a head's first rotary_dim elements is turned by position * inv_freq[i] and scaled by
+ * magnitude (1 unless a long-context scaling asks for another).  Pairs are (i, i + rotary_dim / 2), or (2 i, 2 i + 1)
+ * with interleaved != 0.  d_inv_freq: rotary_dim / 2 floats on the device, any scaling already in them.
+ * 0 <= rotary_dim <= head_dim, a multiple of 16 (of 8 when interleaved); 0: no rotation. */
+typedef struct {
+    const float* d_inv_freq;
+    int32_t rotary_dim, interleaved;
+    float magnitude;
+} jot_rope;
+
+/* Heads of n_rows rows: element (row, head, d) at in + row * in_row_stride + head * in_head_stride + d; `out` may be `in`
+ * with the same strides and must not overlap it otherwise.  gain: head_dim elements (nullable: no norm). */
+typedef struct {
+    const void* in;
+    int64_t in_row_stride, in_head_stride;
+    void* out;
+    int64_t out_row_stride, out_head_stride;
+    const void* gain;
+    int32_t n_heads;
+} jot_heads;
+
+/* Per head of q and k: x * rsqrt(mean(x^2) + eps) * gain (where a gain is given), then the rotation by
+ * d_positions[row] (int32; negative: padding), rounded once.  k may be NULL.  With pages, k's results go to the pages of
+ * `layer` at d_slots[row] = page * page_size + offset (k->out is ignored), and v (not NULL then; in, strides and n_heads
+ * count) is copied beside them; a negative slot writes neither.  Slots must differ: where two rows name one slot,
+ * which of them it holds is not defined.  8 <= head_dim <= 256. */
+int jot_head_norm_rope(const jot_heads* q, const jot_heads* k, const jot_rope* rope, int dtype, int n_rows, int head_dim,
+                       float eps, const int32_t* d_positions, const jot_heads* v, const jot_kv_pages* pages, int layer,
+                       const int32_t* d_slots, int32_t* d_status, void* stream);
+
+/* Rows of keys and values [n_rows, n_kv_heads, head_dim] into the pages of one layer, as above. */
+int jot_kv_write(const jot_kv_pages* pages, int layer, int n_rows, const void* d_k, int64_t k_row_stride,
+                 int64_t k_head_stride, const void* d_v, int64_t v_row_stride, int64_t v_head_stride,
+                 const int32_t* d_slots, int32_t* d_status, void* stream);
+
+/* Page src[i] onto page dst[i], keys and values of every layer.  src and dst are HOST arrays, read before the call
+ * returns.  All pages in [0, n_pages); no page is written twice, and no page is both read and written (JOT_ERR_ARG
+ * otherwise), so the order does not matter: a compaction moves pages from behind the pool's new end into holes before it, a
+ * fork copies a shared page to a fresh one. */
+int jot_kv_copy_pages(const jot_kv_pages* pages, int n, const int32_t* src, const int32_t* dst, void* stream);
+
+/* Attention of T rows per sequence over the sequence's keys in the pages of `layer`: key j of sequence b is in page
+ * d_page_table[b * table_stride + j / page_size] at offset j % page_size, j < d_lens[b].  Every row sees every key
+ * (bidirectional).  q and out [B, T, n_q_heads, head_dim] with strides (sequence, row, head); query head h uses key head
+ * h / (n_q_heads / n_kv_heads).  d_lse (nullable, [B, T, n_q_heads] fp32): ln of the sum of exp(scale * q . k).  A length of 0
+ * gives zeros and -inf.  head_dim 64 or 128.  Entries of a table row past its length are not read.  Tokens past a length within
+ * a page may hold anything, NaN included.
+ * d_workspace: at least jot_paged_attention_workspace_bytes() (0 on invalid arguments), 16-byte aligned, the call's own until it
+ * has finished on the device: two calls (or two graphs) that may run at the same time need one each. */
+size_t jot_paged_attention_workspace_bytes(int T, int n_q_heads, int n_kv_heads, int head_dim);
+int jot_paged_attention(const void* d_q, int64_t q_seq_stride, int64_t q_row_stride, int64_t q_head_stride, void* d_out,
+                        int64_t out_seq_stride, int64_t out_row_stride, int64_t out_head_stride, float* d_lse, int B,
+                        int T, int n_q_heads, const jot_kv_pages* pages, int layer, const int32_t* d_page_table,
+                        int64_t table_stride, int max_pages, const int32_t* d_lens, float scale, void* d_workspace,
+                        size_t workspace_bytes, int32_t* d_status, void* stream);
+
 /* Optional timing of the kernels a model launches, by class, with CUDA events recorded on the launching
  * stream around each launch.  jot_profile(m, 1) starts (and clears) the accumulation, jot_profile(m, 0)
  * stops it; jot_profile_read waits for the recorded events and returns, per class, the accumulated

@@ -22,82 +22,11 @@
 #include "gemm_slab.cuh"
 #include "gemm_stream.cuh"
 #include "glue.cuh"
+#include "host.cuh"
 
 using namespace jot;
 
 namespace {
-
-thread_local int g_last_cuda_error = 0;
-std::atomic<int64_t> g_launches{0};
-
-#define JOT_CUDA(expr)                                  \
-    do {                                                \
-        cudaError_t e_ = (expr);                        \
-        if (e_ != cudaSuccess) {                        \
-            g_last_cuda_error = (int)e_;                \
-            return JOT_ERR_CUDA;                        \
-        }                                               \
-    } while (0)
-#define JOT_TRY(expr)              \
-    do {                           \
-        int s_ = (expr);           \
-        if (s_ != JOT_OK) return s_; \
-    } while (0)
-
-inline int launch_check() {
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) {
-        g_last_cuda_error = (int)e;
-        return JOT_ERR_CUDA;
-    }
-    return JOT_OK;
-}
-
-// Every kernel goes out through here: programmatic stream serialization lets a kernel's launch and
-// on-chip prologue overlap the tail of its predecessor (see pdl.cuh for the device side).
-template <typename... KArgs, typename... Args>
-void launch_k(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);     // errors are picked up by launch_check()
-}
-
-// ---------------------------------------------------------------- device facts
-struct DeviceInfo {
-    int ok = 0, sms = 0, status = JOT_OK;
-    PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
-};
-
-int device_info(DeviceInfo** out) {
-    static thread_local DeviceInfo cache[64];
-    int dev = 0;
-    JOT_CUDA(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return JOT_ERR_DEVICE;
-    DeviceInfo& di = cache[dev];
-    if (!di.ok) {
-        int major = 0;
-        JOT_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
-        JOT_CUDA(cudaDeviceGetAttribute(&di.sms, cudaDevAttrMultiProcessorCount, dev));
-        if (major != 10) return JOT_ERR_DEVICE;
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        JOT_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
-        if (qres != cudaDriverEntryPointSuccess || fn == nullptr) return JOT_ERR_DEVICE;
-        di.encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
-        di.ok = 1;
-    }
-    *out = &di;
-    return JOT_OK;
-}
 
 // bf16 row-major [rows, cols] (row stride ld elements), boxes of 64 columns x box_rows rows, 128-byte swizzle;
 // out-of-range elements read as zero.
@@ -520,8 +449,6 @@ int launch_rmsnorm(const DeviceInfo* di, const __nv_bfloat16* x, const __nv_bflo
     else launch_k(rmsnorm_kernel<8>, grid, block, 0, st, x, gain, out, d, eps, n_rows, rows, d_R);
     return launch_check();
 }
-
-inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 }  // namespace
 

@@ -1,0 +1,480 @@
+// Attention of a few new rows per sequence over the sequence's keys and values in the pages of a cache:
+//
+//   out[b, t, h] = sum_j softmax_j(scale q[b, t, h] . k_j) v_j,   lse[b, t, h] = ln sum_j exp(scale q . k_j),   j < lens[b]
+//
+// key j of sequence b in page table[b, j / page_size] at offset j % page_size.  Bidirectional: no mask but the length.  The
+// rows of one key head (every new row of each of its query heads, row r = t * group + g) share its keys and are worked on
+// together, MT = 16, 32 or 64 at a time.
+//
+// Bound by HBM for few rows (the cache is read once: 2 * head_dim * 2 bytes a key, for R rows 4 R head_dim flops).  Sequences are
+// of any and unequal length, known on the device only, so the work is cut there: all tiles of 64 keys of all (sequence, key
+// head, row tile) items form one line, and CTA i of G takes the tiles [i W / G, (i + 1) W / G) of it, whatever items they belong
+// to.  An item that lies in one CTA's range is finished there; one that spans several leaves, per CTA, the unnormalised fp32
+// output with its maximum and sum, which a second kernel joins.  Nothing is added with atomics: a call gives the same bits every time.
+//
+// A CTA keeps three stages of 64 keys in flight (cp.async, 16 bytes a request, a page table entry fetched one tile ahead); its four
+// warps share a stage as WM warps of 16 rows by 4 / WM ranges of keys, and each range keeps a maximum, a sum and an accumulator of
+// its own until the item ends.  16-byte chunk c of a row sits at position c ^ (row mod 8): eight rows of one chunk are on eight
+// different banks for ldmatrix.  Scores, statistics and accumulators are fp32; probabilities are rounded to the cache's type for
+// the second product (the sum is taken before the rounding).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "heads.cuh"
+#include "ptx.cuh"
+
+namespace jot {
+
+constexpr int kPagedThreads = 128;
+constexpr int kPagedTile = 64;              // keys
+constexpr int kPagedStages = 3;
+constexpr int kPagedMaxCtas = 448;          // three per SM
+
+struct PagedArgs {
+    const void* q;
+    void* out;
+    float* lse;                             // [B, T, nq], nullable
+    int64_t q_b, q_t, q_h, o_b, o_t, o_h;   // strides, elements
+    int B, T, nq, nkv, group;
+    PagesDev pages;
+    const int32_t* table;                   // [B, table_stride], max_pages entries a row
+    int64_t table_stride;
+    int max_pages;
+    const int32_t* lens;                    // [B]; 0: zeros come out; negative: the sequence's rows stay as they were
+    float scale_log2;                       // scale * log2(e)
+    // workspace: one descriptor per CTA, then two partial results per CTA
+    int4* desc;                             // (sequence, item within it, fragments, -) of the item that begins in CTA i and ends in a later one
+    float* partial;                         // [CTA][2][MT][HD] unnormalised outputs
+    float2* partial_ml;                     // [CTA][2][MT] (maximum in base 2, sum)
+    int32_t* status;
+};
+
+template <typename T> struct MmaOp;
+template <> struct MmaOp<__nv_bfloat16> {
+    static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+template <> struct MmaOp<__half> {
+    static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+__device__ __forceinline__ void ldmatrix4(uint32_t* r, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+// 16 bytes global -> shared; without `real` zeros are written and nothing is read
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Keys of sequence b as the kernels count them: within what its table row can name.
+__device__ __forceinline__ int paged_len(const PagedArgs& a, int b) {
+    const int n = a.lens[b];
+    const int64_t most = (int64_t)a.max_pages * a.pages.page_size;
+    return n > most ? (int)most : n;
+}
+
+// Where a CTA's share of the line of tiles begins.
+struct PagedRange {
+    int64_t begin, end, total;      // tiles of the line
+    int ctas;                       // CTAs that have a share
+    int b;                          // sequence of the first tile, and the tile within the sequence
+    int64_t in_seq;
+};
+
+__host__ __device__ __forceinline__ int64_t paged_share(int64_t total, int ctas, int i) { return total * i / ctas; }
+// the CTA that has tile t
+__host__ __device__ __forceinline__ int paged_owner(int64_t total, int ctas, int64_t t) { return (int)(((t + 1) * ctas - 1) / total); }
+
+template <int HD>
+struct PagedSmem {
+    static constexpr int TILE_BYTES = kPagedTile * HD * 2;                       // K or V of one stage
+    static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
+    static constexpr int MERGE_BYTES = 64 * (HD / 4) * 4;                        // WK * MT = 64 rows of a quarter of the columns
+    static constexpr int DYN_BYTES = kPagedStages * STAGE_BYTES + MERGE_BYTES;
+};
+
+template <typename T, int HD, int WM>
+__global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const PagedArgs a) {
+    using SM = PagedSmem<HD>;
+    constexpr int MT = 16 * WM, WK = 4 / WM, KW = kPagedTile / WK;      // rows; ranges of keys; keys of a range
+    constexpr int NT = KW / 8, KS = HD / 16, DT = HD / 8;               // score tiles, steps of the first product, output tiles
+    constexpr int CPR = HD / 8;                                         // 16-byte chunks of a key
+    extern __shared__ __align__(128) uint8_t smem[];
+    float* merge = reinterpret_cast<float*>(smem + kPagedStages * SM::STAGE_BYTES);
+    __shared__ float2 ml[WK][MT];
+    __shared__ int64_t warp_tot[4];
+    __shared__ int found_b;
+    __shared__ int64_t found_in_seq;
+
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int R = a.T * a.group, RT = (R + MT - 1) / MT;
+    const int per_b = a.nkv * RT;                                       // items of a sequence
+
+    // ---- the line of tiles and this CTA's share ----
+    auto tiles_of = [&](int b) -> int64_t {
+        const int n = b < a.B ? paged_len(a, b) : 0;
+        return n > 0 ? (int64_t)((n + kPagedTile - 1) / kPagedTile) * per_b : 0;
+    };
+    PagedRange rg;
+    {
+        int64_t sum = 0;
+        for (int b = tid; b < a.B; b += kPagedThreads) {
+            sum += tiles_of(b);
+            if (blockIdx.x == 0 && a.status && a.lens[b] > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) warp_tot[warp] = sum;
+        __syncthreads();
+        rg.total = warp_tot[0] + warp_tot[1] + warp_tot[2] + warp_tot[3];
+        rg.ctas = (int)min((int64_t)gridDim.x, rg.total);
+        rg.begin = rg.end = 0;
+        if ((int)blockIdx.x < rg.ctas) {
+            rg.begin = paged_share(rg.total, rg.ctas, blockIdx.x);
+            rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
+            int64_t before = 0;
+            for (int b0 = 0; b0 < a.B; b0 += kPagedThreads) {
+                const int64_t mine = tiles_of(b0 + tid);
+                int64_t inc = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+                    if (lane >= o) inc += up;
+                }
+                __syncthreads();                                        // warp_tot is read by everyone before it is written again
+                if (lane == 31) warp_tot[warp] = inc;
+                __syncthreads();
+                int64_t start = before + inc - mine;
+                for (int w = 0; w < warp; ++w) start += warp_tot[w];
+                if (start <= rg.begin && rg.begin < start + mine) {
+                    found_b = b0 + tid;
+                    found_in_seq = rg.begin - start;
+                }
+                before += warp_tot[0] + warp_tot[1] + warp_tot[2] + warp_tot[3];
+                if (before > rg.begin) break;
+            }
+            __syncthreads();
+            rg.b = found_b;
+            rg.in_seq = found_in_seq;
+        }
+    }
+    // sequences without a key: zeros, and the logarithm of nothing
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+        if (a.lens[b] != 0 && !(a.lens[b] > 0 && a.max_pages == 0)) continue;
+        for (int i = tid; i < a.T * a.nq * CPR; i += kPagedThreads) {
+            const int row = i / CPR, t = row / a.nq, h = row - t * a.nq;
+            reinterpret_cast<uint4*>((T*)a.out + b * a.o_b + t * a.o_t + h * a.o_h)[i % CPR] = make_uint4(0, 0, 0, 0);
+            if (i % CPR == 0 && a.lse) a.lse[(int64_t)b * a.T * a.nq + row] = -INFINITY;
+        }
+    }
+    if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if ((int)blockIdx.x >= rg.ctas) return;
+
+    // ---- loads: a walk over the tiles of the share, kPagedStages - 1 ahead of the products ----
+    const uint32_t s0 = smem_u32(smem);
+    int lb = rg.b, ln = paged_len(a, lb), lkt = 0, litem = 0;           // sequence, its keys, tile, item (head * RT + row tile)
+    {
+        const int nt = (ln + kPagedTile - 1) / kPagedTile;
+        litem = (int)(rg.in_seq / nt);
+        lkt = (int)(rg.in_seq - (int64_t)litem * nt);
+    }
+    int64_t lleft = rg.end - rg.begin;
+    const int lrow = warp * 16 + (lane & 15);                           // the tile's row whose page this lane looks up
+    int off = 0;                                                        // its offset within the page
+    auto look_up = [&]() -> int {                                       // page of that row's key in the tile at hand, -1: none
+        const int key = lkt * kPagedTile + lrow;
+        if (lleft <= 0 || key >= ln) return -1;
+        const int p = key / a.pages.page_size;
+        off = key - p * a.pages.page_size;
+        return a.table[lb * a.table_stride + p];
+    };
+    int page = look_up();
+    auto issue = [&](int stage) {
+        if (lleft > 0) {
+            const int head = litem / RT;
+            const bool bad = page < -1 || page >= a.pages.n_pages || (page == -1 && lkt * kPagedTile + lrow < ln);
+            if (bad) {
+                if (a.status) atomicExch(a.status, kStatusBadIndex);
+                page = -1;
+            }
+            const uint32_t sk = s0 + stage * SM::STAGE_BYTES, sv = sk + SM::TILE_BYTES;
+            constexpr int RPP = 32 / CPR;                               // rows per request of a warp
+#pragma unroll
+            for (int i = 0; i < 16 / RPP; ++i) {
+                const int r16 = i * RPP + lane / CPR, c = lane % CPR, r = warp * 16 + r16;
+                const int pg = __shfl_sync(0xffffffffu, page, r16), of = __shfl_sync(0xffffffffu, off, r16);
+                const bool real = pg >= 0;
+                const int64_t in_page = real ? ((int64_t)head * a.pages.page_size + of) * HD + c * 8 : 0;
+                const T* kp = (const T*)a.pages.k + (real ? pg * a.pages.k_page : 0) + in_page;
+                const T* vp = (const T*)a.pages.v + (real ? pg * a.pages.v_page : 0) + in_page;
+                const uint32_t d = (uint32_t)(r * (HD * 2) + ((c ^ (r & 7)) << 4));
+                cp_async16(sk + d, kp, real);
+                cp_async16(sv + d, vp, real);
+            }
+            // next tile
+            --lleft;
+            if ((lkt + 1) * kPagedTile < ln) {
+                ++lkt;
+            } else {
+                lkt = 0;
+                if (++litem == per_b) {
+                    litem = 0;
+                    if (lleft > 0) do { ++lb; ln = paged_len(a, lb); } while (ln <= 0);
+                }
+            }
+            page = look_up();
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kPagedStages - 1; ++s) issue(s);
+
+    // ---- products ----
+    const int wm = warp % WM, wk = warp / WM;
+    const int g = lane >> 2, t4 = lane & 3;
+    int b = rg.b, n = paged_len(a, b), nt = (n + kPagedTile - 1) / kPagedTile;
+    int item = (int)(rg.in_seq / nt), kt = (int)(rg.in_seq - (int64_t)item * nt);
+    int stage = 0;
+    for (int64_t left = rg.end - rg.begin; left > 0;) {
+        const int head = item / RT, row0 = (item - head * RT) * MT;
+        const int kt_first = kt, kt_end = (int)min((int64_t)nt, kt + left);
+        // queries of this warp's 16 rows as operand fragments; rows past R are zeros
+        uint32_t qf[KS][4];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const int r = row0 + wm * 16 + g + 8 * hh, t = r / a.group, gq = r - t * a.group;
+            const T* qp = (const T*)a.q + b * a.q_b + (int64_t)t * a.q_t + (int64_t)(head * a.group + gq) * a.q_h;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                qf[ks][hh] = r < R ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + 2 * t4) : 0u;
+                qf[ks][2 + hh] = r < R ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + 8 + 2 * t4) : 0u;
+            }
+        }
+        float o[DT][4], mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
+
+        for (; kt < kt_end; ++kt, --left) {
+            cp_async_wait<kPagedStages - 2>();
+            __syncthreads();                                            // the tile is there, and the stage before it is free
+            issue(stage == 0 ? kPagedStages - 1 : stage - 1);
+            const uint32_t sk = s0 + stage * SM::STAGE_BYTES, sv = sk + SM::TILE_BYTES;
+            if (++stage == kPagedStages) stage = 0;
+            const int key0 = wk * KW;                                   // first key of this warp's range within the tile
+            float s[NT][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int j = 0; j < NT; j += 2) {
+                    uint32_t kb[4];
+                    const int r = key0 + j * 8 + (lane & 7) + ((lane >> 4) << 3), c = ks * 2 + ((lane >> 3) & 1);
+                    ldmatrix4(kb, sk + r * (HD * 2) + ((c ^ (r & 7)) << 4));
+                    MmaOp<T>::mma(s[j], qf[ks], kb[0], kb[1]);
+                    MmaOp<T>::mma(s[j + 1], qf[ks], kb[2], kb[3]);
+                }
+            const int limit = n - kt * kPagedTile - key0;               // keys of the range that exist
+            float top[2] = {mx[0], mx[1]};
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[j][e] = j * 8 + 2 * t4 + (e & 1) < limit ? s[j][e] * a.scale_log2 : -INFINITY;
+                    top[e >> 1] = fmaxf(top[e >> 1], s[j][e]);
+                }
+            float base[2];
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                top[hh] = fmaxf(top[hh], __shfl_xor_sync(0xffffffffu, top[hh], 1));
+                top[hh] = fmaxf(top[hh], __shfl_xor_sync(0xffffffffu, top[hh], 2));
+                base[hh] = top[hh] == -INFINITY ? 0.f : top[hh];        // no key yet: every exponential is zero against any base
+                const float f = ex2_approx(mx[hh] - base[hh]);
+                mx[hh] = top[hh];
+                sum[hh] *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    o[d][2 * hh] *= f;
+                    o[d][2 * hh + 1] *= f;
+                }
+            }
+            uint32_t p[NT / 2][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                float e[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) e[x] = ex2_approx(s[j][x] - base[x >> 1]);
+                sum[0] += e[0] + e[1];
+                sum[1] += e[2] + e[3];
+                typename Pack2<T>::type lo = Pack2<T>::down(e[0], e[1]), hi = Pack2<T>::down(e[2], e[3]);
+                p[j >> 1][(j & 1) * 2] = *reinterpret_cast<uint32_t*>(&lo);
+                p[j >> 1][(j & 1) * 2 + 1] = *reinterpret_cast<uint32_t*>(&hi);
+            }
+#pragma unroll
+            for (int j = 0; j < NT / 2; ++j)
+#pragma unroll
+                for (int d = 0; d < DT; d += 2) {
+                    uint32_t vb[4];
+                    const int r = key0 + j * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), c = d + (lane >> 4);
+                    ldmatrix4_trans(vb, sv + r * (HD * 2) + ((c ^ (r & 7)) << 4));
+                    MmaOp<T>::mma(o[d], p[j], vb[0], vb[1]);
+                    MmaOp<T>::mma(o[d + 1], p[j], vb[2], vb[3]);
+                }
+        }
+
+        // ---- the ranges of keys meet; the item, or this CTA's part of it, goes out ----
+        const bool begins = kt_first == 0, ends = kt_end == nt;
+        const int slot = (int)blockIdx.x * 2 + (begins ? 1 : 0);
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            sum[hh] += __shfl_xor_sync(0xffffffffu, sum[hh], 1);
+            sum[hh] += __shfl_xor_sync(0xffffffffu, sum[hh], 2);
+            if (t4 == 0) ml[wk][wm * 16 + g + 8 * hh] = make_float2(mx[hh], sum[hh]);
+        }
+        __syncthreads();
+        float mine[2];                                                  // what this warp's accumulators are multiplied by
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) m = fmaxf(m, ml[w][wm * 16 + g + 8 * hh].x);
+            mine[hh] = m == -INFINITY ? 1.f : ex2_approx(mx[hh] - m);
+        }
+        auto totals = [&](int r, float& m, float& l) {
+            m = -INFINITY;
+            l = 0.f;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) m = fmaxf(m, ml[w][r].x);
+#pragma unroll
+            for (int w = 0; w < WK; ++w) l += ml[w][r].y * (m == -INFINITY ? 1.f : ex2_approx(ml[w][r].x - m));
+        };
+        if (tid < MT && row0 + tid < R) {
+            float m, l;
+            totals(tid, m, l);
+            const int r = row0 + tid, t = r / a.group, gq = r - t * a.group;
+            if (begins && ends) {
+                if (a.lse) a.lse[((int64_t)b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(l)) * 0.69314718055994531f;
+            } else {
+                a.partial_ml[(int64_t)slot * MT + tid] = make_float2(m, l);
+            }
+        }
+        constexpr int QC = HD / 4, QD = DT / 4;                         // columns and output tiles of a quarter
+#pragma unroll
+        for (int quarter = 0; quarter < 4; ++quarter) {
+#pragma unroll
+            for (int d = 0; d < QD; ++d)
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh)
+                    *reinterpret_cast<float2*>(merge + ((wk * MT + wm * 16 + g + 8 * hh) * QC + d * 8 + 2 * t4)) =
+                        make_float2(o[quarter * QD + d][2 * hh] * mine[hh], o[quarter * QD + d][2 * hh + 1] * mine[hh]);
+            __syncthreads();
+            for (int i = tid; i < MT * (QC / 8); i += kPagedThreads) {
+                const int r = i / (QC / 8), c = (i % (QC / 8)) * 8;
+                if (row0 + r >= R) continue;
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < WK; ++w)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] += merge[(w * MT + r) * QC + c + e];
+                if (begins && ends) {
+                    float m, l;
+                    totals(r, m, l);
+                    const float inv = 1.f / l;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] *= inv;
+                    const int rr = row0 + r, t = rr / a.group, gq = rr - t * a.group;
+                    *reinterpret_cast<uint4*>((T*)a.out + b * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + quarter * QC + c) = pack8<T>(x);
+                } else {
+                    float4* dst = reinterpret_cast<float4*>(a.partial + ((int64_t)slot * MT + r) * HD + quarter * QC + c);
+                    dst[0] = make_float4(x[0], x[1], x[2], x[3]);
+                    dst[1] = make_float4(x[4], x[5], x[6], x[7]);
+                }
+            }
+            __syncthreads();
+        }
+        if (begins && !ends && tid == 0) {
+            // tiles of the line from the item's first to its last; the next CTAs have the rest of them
+            const int64_t last = rg.end + (nt - kt_end) - 1;
+            a.desc[blockIdx.x] = make_int4(b, item, paged_owner(rg.total, rg.ctas, last) - (int)blockIdx.x + 1, 0);
+        }
+        // next item
+        kt = 0;
+        if (++item == per_b && left > 0) {
+            item = 0;
+            do { ++b; n = paged_len(a, b); } while (n <= 0);
+            nt = (n + kPagedTile - 1) / kPagedTile;
+        }
+    }
+    cp_async_wait<0>();
+}
+
+// Joins the parts of the items that several CTAs worked on: one CTA per (CTA in which an item begins, row), each warp a share of the
+// parts, a lane HD / 32 columns.
+template <typename T, int HD>
+__global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedArgs a, int MT) {
+    grid_launch_dependents();
+    grid_dependency_wait();
+    constexpr int E = HD / 32;
+    __shared__ float so[4][HD];
+    __shared__ float2 sml[4];
+    const int4 d = a.desc[blockIdx.x];
+    if (d.z == 0) return;
+    const int R = a.T * a.group, RT = (R + MT - 1) / MT;
+    const int head = d.y / RT, row0 = (d.y - head * RT) * MT, r = blockIdx.y;
+    if (row0 + r >= R) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float m = -INFINITY, l = 0.f, o[E] = {};
+    for (int f = warp; f < d.z; f += 4) {
+        const int64_t slot = f == 0 ? (int64_t)blockIdx.x * 2 + 1 : (int64_t)(blockIdx.x + f) * 2;
+        const float2 p = a.partial_ml[slot * MT + r];
+        float x[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = a.partial[(slot * MT + r) * HD + lane * E + e];
+        const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
+        const float fo = ex2_approx(m - base), fn = ex2_approx(p.x - base);
+        m = top;
+        l = l * fo + p.y * fn;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = o[e] * fo + x[e] * fn;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) so[warp][lane * E + e] = o[e];
+    if (lane == 0) sml[warp] = make_float2(m, l);
+    __syncthreads();
+    if (threadIdx.x >= HD / 8) return;
+    float top = -INFINITY, total = 0.f, x[8] = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, sml[w].x);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = top == -INFINITY ? 1.f : ex2_approx(sml[w].x - top);
+        total += sml[w].y * f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += so[w][threadIdx.x * 8 + e] * f;
+    }
+    const float inv = 1.f / total;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    const int rr = row0 + r, t = rr / a.group, gq = rr - t * a.group;
+    reinterpret_cast<uint4*>((T*)a.out + d.x * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h)[threadIdx.x] = pack8<T>(x);
+    if (threadIdx.x == 0 && a.lse) a.lse[((int64_t)d.x * a.T + t) * a.nq + head * a.group + gq] = (top + log2f(total)) * 0.69314718055994531f;
+}
+
+}  // namespace jot

@@ -8,6 +8,8 @@ from __future__ import annotations
 
 import ctypes as C
 import dataclasses
+import functools
+import math
 import os
 from typing import List, Optional, Sequence
 
@@ -22,7 +24,8 @@ EXPORTS = [
     "jot_launch_count", "jot_profile", "jot_profile_read", "jot_gemm_bf16_noalloc",
     "jot_selftest_wait_expiry", "jot_kv_cache_bytes", "jot_attach_kv_cache", "jot_denoise_step_cached",
     "jot_max_active_rows", "jot_lm_head_partition", "jot_set_sync", "jot_read_status",
-    "jot_lm_head_stats_slice", "jot_merge_stats",
+    "jot_lm_head_stats_slice", "jot_merge_stats", "jot_head_norm_rope", "jot_kv_write", "jot_kv_copy_pages",
+    "jot_paged_attention", "jot_paged_attention_workspace_bytes",
 ]
 
 NOALLOC_SCRATCH_BYTES = 16 << 20
@@ -84,6 +87,21 @@ class _Trace(C.Structure):
                 ("n_candidates", C.c_void_p)]
 
 
+class _KVPages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_layer_stride", C.c_int64), ("v_layer_stride", C.c_int64),
+                ("k_page_stride", C.c_int64), ("v_page_stride", C.c_int64), ("n_layers", C.c_int32), ("n_pages", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float)]
+
+
+class _Heads(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("in_row_stride", C.c_int64), ("in_head_stride", C.c_int64), ("out", C.c_void_p),
+                ("out_row_stride", C.c_int64), ("out_head_stride", C.c_int64), ("gain", C.c_void_p), ("n_heads", C.c_int32)]
+
+
 @dataclasses.dataclass
 class Trace:
     """Optional per-position / per-step record of a generation (device tensors)."""
@@ -143,6 +161,17 @@ def _lib():
         lib.jot_read_status.argtypes = [C.c_void_p, C.c_void_p]
         lib.jot_profile.argtypes = [C.c_void_p, C.c_int]
         lib.jot_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.c_int]
+        heads, pages = C.POINTER(_Heads), C.POINTER(_KVPages)
+        lib.jot_head_norm_rope.argtypes = [heads, heads, C.POINTER(_Rope), C.c_int, C.c_int, C.c_int, C.c_float, C.c_void_p,
+                                           heads, pages, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.jot_kv_write.argtypes = [pages, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64,
+                                     C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.jot_kv_copy_pages.argtypes = [pages, C.c_int, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_void_p]
+        lib.jot_paged_attention_workspace_bytes.restype = C.c_size_t
+        lib.jot_paged_attention_workspace_bytes.argtypes = [C.c_int] * 4
+        lib.jot_paged_attention.argtypes = ([C.c_void_p, C.c_int64, C.c_int64, C.c_int64] * 2 + [C.c_void_p] + [C.c_int] * 3
+                                            + [pages, C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_float,
+                                               C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p])
         _LIB = lib
     return _LIB
 
@@ -459,3 +488,205 @@ def selftest_wait_expiry(limit_ns: int = 20_000_000) -> int:
     status = torch.full((1,), -1, dtype=torch.int32, device="cuda")
     _check(_lib().jot_selftest_wait_expiry(status.data_ptr(), limit_ns, _stream()), "jot_selftest_wait_expiry")
     return int(status.item())
+
+
+# ---- decoding over a paged key-value cache -----------------------------------------------------------------------------
+_ELEMENTS = {torch.bfloat16: 0, torch.float16: 1}     # JOT_BF16, JOT_FP16
+STATUS_BAD_INDEX = 6                                    # what a status word becomes: a slot, page or length outside the pages
+
+
+def _launch(device, where: str, fn, *args) -> None:
+    """fn(*args, stream) on the current stream of the tensors' own device, whichever device is current."""
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+
+
+def _int_ptr(t: Optional[torch.Tensor], name: str, device, shape) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous int32 tensor on {device}, got {t.dtype} on {t.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _element_tensor(t: torch.Tensor, name: str, dtype, device, dims: int) -> None:
+    if not t.is_cuda or t.device != device or t.dtype != dtype or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise TypeError(f"{name}: expected a {dims}-D {dtype} tensor on {device} whose last dimension is contiguous, got "
+                        f"{t.dim()}-D {t.dtype} on {t.device} with strides {t.stride()}")
+
+
+class KVPages:
+    """The pages of a key-value cache: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim], bf16 or fp16.  A page
+    (its last three dimensions) is contiguous; layers and pages may lie at any stride that is a multiple of 8 elements, so
+    that k and v may be two halves of one tensor.  The tensors are borrowed and written in place."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _ELEMENTS or not k.is_cuda or k.device != v.device:
+            raise TypeError("KVPages: k and v must be CUDA tensors [n_layers, n_pages, n_kv_heads, page_size, head_dim] of one "
+                            "shape and device, bf16 or fp16")
+        n_layers, n_pages, n_kv_heads, page_size, head_dim = k.shape
+        for t in (k, v):
+            if not (t.numel() == 0 or t[0, 0].is_contiguous()):
+                raise TypeError("KVPages: the last three dimensions must be contiguous")
+        self.k, self.v = k, v
+        self.device, self.dtype = k.device, k.dtype
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self._c = _KVPages(k.data_ptr(), v.data_ptr(), k.stride(0), v.stride(0), k.stride(1), v.stride(1), n_layers, n_pages,
+                           n_kv_heads, page_size, head_dim, _ELEMENTS[k.dtype])
+
+    @staticmethod
+    def empty(n_layers: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype=torch.bfloat16,
+              device="cuda") -> "KVPages":
+        shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+        return KVPages(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
+
+
+@dataclasses.dataclass
+class Rope:
+    """A position rotation: inv_freq [rotary_dim / 2] (fp32, on the device, any long-context scaling already in it), pairs
+    (i, i + rotary_dim / 2) or neighbours, cos and sin times `magnitude`."""
+    inv_freq: torch.Tensor
+    interleaved: bool = False
+    magnitude: float = 1.0
+
+
+def rope_frequencies(rotary_dim: int, theta: float, factor: float = 1.0, original_len: Optional[int] = None,
+                     low_turns: float = 1.0, high_turns: float = 4.0, device="cuda") -> torch.Tensor:
+    """Frequencies theta^(-2 i / rotary_dim) of a rotation, made in float64 and rounded to float32.
+
+    For contexts `factor` times as long as the model was trained on: without original_len every frequency is divided by
+    the factor (positions interpolated); with it, pairs that make at least high_turns turns over original_len positions keep
+    their frequency, pairs that make at most low_turns are divided by the factor, and in between the two are blended
+    linearly in the number of turns."""
+    if rotary_dim <= 0 or rotary_dim % 2 or not theta > 0 or not factor > 0:
+        raise ValueError("rope_frequencies: rotary_dim must be positive and even, theta and factor positive")
+    f = float(theta) ** (-2.0 * torch.arange(rotary_dim // 2, dtype=torch.float64) / rotary_dim)
+    keep = torch.zeros_like(f)
+    if original_len is not None:
+        if not high_turns > low_turns:
+            raise ValueError("rope_frequencies: high_turns must exceed low_turns")
+        keep = ((original_len * f / (2.0 * math.pi) - low_turns) / (high_turns - low_turns)).clamp(0.0, 1.0)
+    return (f * (keep + (1.0 - keep) / factor)).to(torch.float32).to(device)
+
+
+def _heads(x: torch.Tensor, out: Optional[torch.Tensor], gain: Optional[torch.Tensor], name: str, device, dtype, rows, hd) -> _Heads:
+    _element_tensor(x, name, dtype, device, 3)
+    if x.shape[0] != rows or x.shape[2] != hd:
+        raise ValueError(f"{name}: expected [{rows}, heads, {hd}], got {tuple(x.shape)}")
+    h = _Heads(x.data_ptr(), x.stride(0), x.stride(1), None, 0, 0, None, x.shape[1])
+    if out is not None:
+        _element_tensor(out, name + "_out", dtype, device, 3)
+        if out.shape != x.shape:
+            raise ValueError(f"{name}_out: expected shape {tuple(x.shape)}, got {tuple(out.shape)}")
+        h.out, h.out_row_stride, h.out_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
+    if gain is not None:
+        if gain.dtype != dtype or gain.device != device or gain.shape != (hd,) or not gain.is_contiguous():
+            raise TypeError(f"{name}_gain: expected a contiguous {dtype} tensor [{hd}] on {device}")
+        h.gain = gain.data_ptr()
+    return h
+
+
+def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, rope: Rope,
+                   q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, *,
+                   q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                   v: Optional[torch.Tensor] = None, pages: Optional[KVPages] = None, layer: int = 0,
+                   slots: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Norm of every head of q [rows, heads, head_dim] and k (where a gain is given), then the rotation by positions [rows]
+    (int32), in one pass.  Returns (q_out, k_out): new tensors unless given (q itself: in place).  With pages, k's results and
+    v go to `layer` of the pages at slots [rows] = page * page_size + offset (int32), and k_out is None.  A row with a
+    negative position, and the pages of a row with a negative slot, stay as they were."""
+    device, dtype = q.device, q.dtype
+    if dtype not in _ELEMENTS or q.dim() != 3:
+        raise TypeError(f"q: expected a 3-D bf16 or fp16 tensor, got {q.dim()}-D {dtype}")
+    rows, _, hd = q.shape
+    f = rope.inv_freq
+    if f.dtype != torch.float32 or f.device != device or f.dim() != 1 or not f.is_contiguous():
+        raise TypeError(f"rope.inv_freq: expected a contiguous 1-D float32 tensor on {device}")
+    if pages is not None and (k is None or v is None or slots is None or k_out is not None):
+        raise ValueError("head_norm_rope: pages need k, v and slots, and take the place of k_out")
+    if pages is None and (v is not None or slots is not None):
+        raise ValueError("head_norm_rope: v and slots go with pages")
+    if pages is not None and pages.device != device:
+        raise TypeError(f"pages: expected on {device}, got {pages.device}")
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=dtype, device=device)
+    if k is not None and pages is None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=dtype, device=device)
+    hq = _heads(q, q_out, q_gain, "q", device, dtype, rows, hd)
+    hk = None if k is None else C.byref(_heads(k, k_out, k_gain, "k", device, dtype, rows, hd))
+    hv = None if v is None else C.byref(_heads(v, None, None, "v", device, dtype, rows, hd))
+    r = _Rope(f.data_ptr(), 2 * f.numel(), int(rope.interleaved), rope.magnitude)
+    _launch(device, "jot_head_norm_rope", _lib().jot_head_norm_rope, C.byref(hq), hk, C.byref(r), _ELEMENTS[dtype], rows, hd, eps,
+            _int_ptr(positions, "positions", device, (rows,)), hv, None if pages is None else C.byref(pages._c), layer,
+            _int_ptr(slots, "slots", device, (rows,)), _int_ptr(status, "status", device, (1,)))
+    return q_out, k_out
+
+
+def kv_write(pages: KVPages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, layer: int = 0,
+             status: Optional[torch.Tensor] = None) -> None:
+    """Rows k, v [rows, n_kv_heads, head_dim] into `layer` of the pages at slots [rows] (int32; negative: skipped).  Slots must
+    differ from each other."""
+    shape = (k.shape[0], pages.n_kv_heads, pages.head_dim)
+    for t, name in ((k, "k"), (v, "v")):
+        _element_tensor(t, name, pages.dtype, pages.device, 3)
+        if t.shape != shape:
+            raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    _launch(pages.device, "jot_kv_write", _lib().jot_kv_write, C.byref(pages._c), layer, k.shape[0], k.data_ptr(), k.stride(0),
+            k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), _int_ptr(slots, "slots", pages.device, (k.shape[0],)),
+            _int_ptr(status, "status", pages.device, (1,)))
+
+
+def kv_copy_pages(pages: KVPages, src: Sequence[int], dst: Sequence[int]) -> None:
+    """Page src[i] onto page dst[i], in every layer.  src and dst are lists on the host; no page twice in dst, none in both."""
+    if len(src) != len(dst):
+        raise ValueError("kv_copy_pages: src and dst differ in length")
+    n = len(src)
+    pair = C.c_int32 * n
+    _launch(pages.device, "jot_kv_copy_pages", _lib().jot_kv_copy_pages, C.byref(pages._c), n, pair(*src), pair(*dst))
+
+
+@functools.lru_cache(maxsize=None)
+def paged_attention_workspace_bytes(T: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    """Device bytes a paged_attention call of T rows a sequence needs, whatever the batch and the lengths (0: unsupported)."""
+    return int(_lib().jot_paged_attention_workspace_bytes(T, n_q_heads, n_kv_heads, head_dim))
+
+
+def paged_attention(q: torch.Tensor, pages: KVPages, page_table: torch.Tensor, lens: torch.Tensor, layer: int = 0,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of q [B, T, n_q_heads, head_dim] over the first lens[b] keys of each sequence, which lie in the pages of
+    `layer` that page_table [B, max_pages] names (both int32).  Bidirectional: every row sees every key.  scale defaults to
+    head_dim^-0.5; lse [B, T, n_q_heads] (fp32, optional) receives the logarithm of the sum of exponentials.  A length of 0
+    gives zeros and -inf, a negative one leaves its sequence's rows of out and lse as they were.
+
+    workspace: optional uint8 tensor of paged_attention_workspace_bytes(); calls that may overlap need one each."""
+    device = pages.device
+    _element_tensor(q, "q", pages.dtype, device, 4)
+    B, T, nq, hd = q.shape
+    if hd != pages.head_dim:
+        raise ValueError(f"q: expected heads of {pages.head_dim}, got {hd}")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=device)
+    else:
+        _element_tensor(out, "out", pages.dtype, device, 4)
+        if out.shape != q.shape:
+            raise ValueError(f"out: expected shape {tuple(q.shape)}, got {tuple(out.shape)}")
+    if lse is not None and (lse.dtype != torch.float32 or lse.device != device or lse.shape != q.shape[:3] or not lse.is_contiguous()):
+        raise TypeError(f"lse: expected a contiguous float32 tensor {tuple(q.shape[:3])} on {device}")
+    if page_table.dtype != torch.int32 or page_table.device != device or page_table.dim() != 2 or page_table.shape[0] != B or (
+            page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise TypeError(f"page_table: expected an int32 tensor [{B}, max_pages] on {device} with contiguous rows")
+    if workspace is None:
+        workspace = torch.empty(paged_attention_workspace_bytes(T, nq, pages.n_kv_heads, hd), dtype=torch.uint8, device=device)
+    elif workspace.dtype != torch.uint8 or workspace.device != device or not workspace.is_contiguous():
+        raise TypeError(f"workspace: expected a contiguous uint8 tensor on {device}")
+    _launch(device, "jot_paged_attention", _lib().jot_paged_attention, q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), out.data_ptr(),
+            out.stride(0), out.stride(1), out.stride(2), None if lse is None else lse.data_ptr(), B, T, nq, C.byref(pages._c), layer,
+            page_table.data_ptr(), page_table.stride(0), page_table.shape[1], _int_ptr(lens, "lens", device, (B,)),
+            hd ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel(), _int_ptr(status, "status", device, (1,)))
+    return out
