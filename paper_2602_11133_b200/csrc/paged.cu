@@ -130,7 +130,10 @@ int launch_paged_t(const DeviceInfo* di, const PagedArgs& a, int64_t most_tiles,
     launch_k(kernel, dim3((unsigned)grid), dim3(kPagedThreads), smem, st, a);
     JOT_TRY(launch_check());
     if (one_tile) return JOT_OK;                                        // an item of one tile is never in two CTAs
-    launch_k((paged_join_kernel<T, HD>), dim3((unsigned)grid, (unsigned)std::min(16 * WM, a.T * a.group)), dim3(kPagedThreads), 0, st, a, 16 * WM);
+    // Four warps to a row where an item may be in many parts (few items on many CTAs), a warp to a row otherwise.
+    const int rows = std::min(16 * WM, a.T * a.group), row_tiles = (a.T * a.group + 16 * WM - 1) / (16 * WM);
+    if (grid > 8ll * a.B * a.nkv * row_tiles) launch_k((paged_join_kernel<T, HD, 1>), dim3((unsigned)grid, (unsigned)rows), dim3(kPagedThreads), 0, st, a, 16 * WM);
+    else launch_k((paged_join_kernel<T, HD, 4>), dim3((unsigned)grid, (unsigned)((rows + 3) / 4)), dim3(kPagedThreads), 0, st, a, 16 * WM);
     return launch_check();
 }
 

@@ -115,6 +115,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     extern __shared__ __align__(128) uint8_t smem[];
     float* merge = reinterpret_cast<float*>(smem + kPagedStages * SM::STAGE_BYTES);
     __shared__ float2 ml[WK][MT];
+    __shared__ uint64_t row_at[2][2 * kPagedTile];                      // addresses of a tile's key rows, then of its value rows
     __shared__ int64_t warp_tot[4];
     __shared__ int found_b;
     __shared__ int64_t found_in_seq;
@@ -185,68 +186,94 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if ((int)blockIdx.x >= rg.ctas) return;
 
-    // ---- loads: a walk over the tiles of the share, kPagedStages - 1 ahead of the products ----
+    // ---- loads: a walk over the tiles of the share ----
+    // Three steps a tile, each one tile behind the one before: a page table entry is requested; the addresses of a key and of a
+    // value row are left in shared memory (thread i < 64: key i, thread 64 + i: value i); the tile is requested.  So no step
+    // waits for the one it needs, and a request costs a thread one shared-memory read and one add.
     const uint32_t s0 = smem_u32(smem);
-    int lb = rg.b, ln = paged_len(a, lb), lkt = 0, litem = 0;           // sequence, its keys, tile, item (head * RT + row tile)
+    int lb = rg.b, ln = paged_len(a, lb), lkt, litem;                   // sequence, its keys, tile, item (head * RT + row tile)
     {
         const int nt = (ln + kPagedTile - 1) / kPagedTile;
         litem = (int)(rg.in_seq / nt);
         lkt = (int)(rg.in_seq - (int64_t)litem * nt);
     }
-    int64_t lleft = rg.end - rg.begin;
-    const int lrow = warp * 16 + (lane & 15);                           // the tile's row whose page this lane looks up
-    int off = 0;                                                        // its offset within the page
-    auto look_up = [&]() -> int {                                       // page of that row's key in the tile at hand, -1: none
-        const int key = lkt * kPagedTile + lrow;
-        if (lleft <= 0 || key >= ln) return -1;
-        const int p = key / a.pages.page_size;
-        off = key - p * a.pages.page_size;
-        return a.table[lb * a.table_stride + p];
-    };
-    int page = look_up();
-    auto issue = [&](int stage) {
-        if (lleft > 0) {
-            const int head = litem / RT;
-            const bool bad = page < -1 || page >= a.pages.n_pages || (page == -1 && lkt * kPagedTile + lrow < ln);
-            if (bad) {
-                if (a.status) atomicExch(a.status, kStatusBadIndex);
-                page = -1;
-            }
-            const uint32_t sk = s0 + stage * SM::STAGE_BYTES, sv = sk + SM::TILE_BYTES;
-            constexpr int RPP = 32 / CPR;                               // rows per request of a warp
-#pragma unroll
-            for (int i = 0; i < 16 / RPP; ++i) {
-                const int r16 = i * RPP + lane / CPR, c = lane % CPR, r = warp * 16 + r16;
-                const int pg = __shfl_sync(0xffffffffu, page, r16), of = __shfl_sync(0xffffffffu, off, r16);
-                const bool real = pg >= 0;
-                const int64_t in_page = real ? ((int64_t)head * a.pages.page_size + of) * HD + c * 8 : 0;
-                const T* kp = (const T*)a.pages.k + (real ? pg * a.pages.k_page : 0) + in_page;
-                const T* vp = (const T*)a.pages.v + (real ? pg * a.pages.v_page : 0) + in_page;
-                const uint32_t d = (uint32_t)(r * (HD * 2) + ((c ^ (r & 7)) << 4));
-                cp_async16(sk + d, kp, real);
-                cp_async16(sv + d, vp, real);
-            }
-            // next tile
-            --lleft;
-            if ((lkt + 1) * kPagedTile < ln) {
-                ++lkt;
-            } else {
-                lkt = 0;
-                if (++litem == per_b) {
-                    litem = 0;
-                    if (lleft > 0) do { ++lb; ln = paged_len(a, lb); } while (ln <= 0);
-                }
-            }
-            page = look_up();
+    int64_t lleft = rg.end - rg.begin;                                  // tiles whose table entry is yet to be requested
+    const int64_t page_stride = tid < kPagedTile ? a.pages.k_page : a.pages.v_page;
+    const T* const pages = (const T*)(tid < kPagedTile ? a.pages.k : a.pages.v);
+    int page = 0, in_page = 0;                                          // of this thread's row in the tile last requested; -1: no such key
+    bool exists = false;
+    auto request_entry = [&]() {
+        exists = false;
+        if (lleft <= 0) return;
+        const int key = lkt * kPagedTile + (tid & (kPagedTile - 1));
+        if (key < ln) {
+            const int p = key / a.pages.page_size;
+            in_page = (litem / RT) * a.pages.page_size + key - p * a.pages.page_size;
+            page = a.table[lb * a.table_stride + p];
+            exists = true;
         }
-        cp_async_commit();
+        --lleft;
+        if ((lkt + 1) * kPagedTile < ln) {
+            ++lkt;
+        } else {
+            lkt = 0;
+            if (++litem == per_b) {
+                litem = 0;
+                if (lleft > 0) do { ++lb; ln = paged_len(a, lb); } while (ln <= 0);
+            }
+        }
     };
+    auto leave_address = [&](int buf) {                                 // an odd address: no such row, zeros are written
+        uint64_t at = reinterpret_cast<uint64_t>(pages) | 1u;
+        if (exists) {
+            if ((unsigned)page < (unsigned)a.pages.n_pages)
+                at = reinterpret_cast<uint64_t>(pages + page * page_stride + (int64_t)in_page * HD);
+            else if (a.status)
+                atomicExch(a.status, kStatusBadIndex);
+        }
+        row_at[buf][tid] = at;
+    };
+    constexpr int RPP = 32 / CPR;                                       // rows per request of a warp
+    const int lr = lane / CPR, lc = lane % CPR;
+    uint32_t ldst[8 / RPP];                                             // where this lane's chunk goes: repeats every 8 rows
 #pragma unroll
-    for (int s = 0; s < kPagedStages - 1; ++s) issue(s);
+    for (int i = 0; i < 8 / RPP; ++i) ldst[i] = (uint32_t)((warp * 16 + i * RPP + lr) * (HD * 2) + ((lc ^ ((i * RPP + lr) & 7)) << 4));
+    auto request_tile = [&](int stage, int buf) {
+        const uint32_t sk = s0 + stage * SM::STAGE_BYTES;
+#pragma unroll
+        for (int i = 0; i < 16 / RPP; ++i) {
+            const int r = warp * 16 + i * RPP + lr;
+            const uint32_t d = sk + ldst[i % (8 / RPP)] + (i * RPP / 8) * 8 * (HD * 2);
+            const uint64_t kp = row_at[buf][r], vp = row_at[buf][kPagedTile + r];
+            cp_async16(d, reinterpret_cast<const uint8_t*>(kp & ~1ull) + lc * 16, !(kp & 1));
+            cp_async16(d + SM::TILE_BYTES, reinterpret_cast<const uint8_t*>(vp & ~1ull) + lc * 16, !(vp & 1));
+        }
+    };
+    const int64_t share = rg.end - rg.begin;
+    int64_t requested = 0;                                              // tiles
+    request_entry();
+    leave_address(0);
+    request_entry();
+#pragma unroll
+    for (int s = 0; s < kPagedStages - 1; ++s) {
+        __syncthreads();
+        if (requested < share) request_tile(s, s & 1);
+        cp_async_commit();
+        ++requested;
+        leave_address((s + 1) & 1);
+        request_entry();
+    }
 
     // ---- products ----
     const int wm = warp % WM, wk = warp / WM;
     const int g = lane >> 2, t4 = lane & 3;
+    // operand addresses within a tile: a lane's row, and the swizzled position of chunk 2 i (+ 1) for i < 4; the next four lie 128 bytes on
+    uint32_t kofs[4], vofs[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        kofs[i] = (uint32_t)(((lane & 7) + ((lane >> 4) << 3)) * (HD * 2) + (((2 * i + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
+        vofs[i] = (uint32_t)(((lane & 7) + (((lane >> 3) & 1) << 3)) * (HD * 2) + (((2 * i + (lane >> 4)) ^ (lane & 7)) << 4));
+    }
     int b = rg.b, n = paged_len(a, b), nt = (n + kPagedTile - 1) / kPagedTile;
     int item = (int)(rg.in_seq / nt), kt = (int)(rg.in_seq - (int64_t)item * nt);
     int stage = 0;
@@ -272,10 +299,13 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
         for (; kt < kt_end; ++kt, --left) {
             cp_async_wait<kPagedStages - 2>();
             __syncthreads();                                            // the tile is there, and the stage before it is free
-            issue(stage == 0 ? kPagedStages - 1 : stage - 1);
-            const uint32_t sk = s0 + stage * SM::STAGE_BYTES, sv = sk + SM::TILE_BYTES;
+            if (requested < share) request_tile(stage == 0 ? kPagedStages - 1 : stage - 1, (int)(requested & 1));
+            cp_async_commit();
+            ++requested;
+            leave_address((int)(requested & 1));
+            request_entry();
+            const uint32_t sk = s0 + stage * SM::STAGE_BYTES + wk * KW * (HD * 2), sv = sk + SM::TILE_BYTES;
             if (++stage == kPagedStages) stage = 0;
-            const int key0 = wk * KW;                                   // first key of this warp's range within the tile
             float s[NT][4];
 #pragma unroll
             for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
@@ -284,33 +314,44 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
 #pragma unroll
                 for (int j = 0; j < NT; j += 2) {
                     uint32_t kb[4];
-                    const int r = key0 + j * 8 + (lane & 7) + ((lane >> 4) << 3), c = ks * 2 + ((lane >> 3) & 1);
-                    ldmatrix4(kb, sk + r * (HD * 2) + ((c ^ (r & 7)) << 4));
+                    ldmatrix4(kb, sk + kofs[ks % 4] + (ks / 4) * 128 + j * 8 * (HD * 2));
                     MmaOp<T>::mma(s[j], qf[ks], kb[0], kb[1]);
                     MmaOp<T>::mma(s[j + 1], qf[ks], kb[2], kb[3]);
                 }
-            const int limit = n - kt * kPagedTile - key0;               // keys of the range that exist
+            const int limit = n - kt * kPagedTile - wk * KW;            // keys of the range that exist
             float top[2] = {mx[0], mx[1]};
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[j][e] = j * 8 + 2 * t4 + (e & 1) < limit ? s[j][e] * a.scale_log2 : -INFINITY;
-                    top[e >> 1] = fmaxf(top[e >> 1], s[j][e]);
-                }
-            float base[2];
+                for (int e = 0; e < 4; ++e) s[j][e] *= a.scale_log2;
+            if (limit < KW) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (j * 8 + 2 * t4 + (e & 1) >= limit) s[j][e] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top[e >> 1] = fmaxf(top[e >> 1], s[j][e]);
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
                 top[hh] = fmaxf(top[hh], __shfl_xor_sync(0xffffffffu, top[hh], 1));
                 top[hh] = fmaxf(top[hh], __shfl_xor_sync(0xffffffffu, top[hh], 2));
-                base[hh] = top[hh] == -INFINITY ? 0.f : top[hh];        // no key yet: every exponential is zero against any base
-                const float f = ex2_approx(mx[hh] - base[hh]);
-                mx[hh] = top[hh];
-                sum[hh] *= f;
+            }
+            float base[2] = {top[0] == -INFINITY ? 0.f : top[0], top[1] == -INFINITY ? 0.f : top[1]};   // no key yet: all exponentials are zero
+            if (__any_sync(0xffffffffu, top[0] != mx[0] || top[1] != mx[1])) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    o[d][2 * hh] *= f;
-                    o[d][2 * hh + 1] *= f;
+                for (int hh = 0; hh < 2; ++hh) {
+                    const float f = ex2_approx(mx[hh] - base[hh]);
+                    mx[hh] = top[hh];
+                    sum[hh] *= f;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        o[d][2 * hh] *= f;
+                        o[d][2 * hh + 1] *= f;
+                    }
                 }
             }
             uint32_t p[NT / 2][4];
@@ -330,8 +371,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
 #pragma unroll
                 for (int d = 0; d < DT; d += 2) {
                     uint32_t vb[4];
-                    const int r = key0 + j * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), c = d + (lane >> 4);
-                    ldmatrix4_trans(vb, sv + r * (HD * 2) + ((c ^ (r & 7)) << 4));
+                    ldmatrix4_trans(vb, sv + vofs[d / 2 % 4] + (d / 8) * 128 + j * 16 * (HD * 2));
                     MmaOp<T>::mma(o[d], p[j], vb[0], vb[1]);
                     MmaOp<T>::mma(o[d + 1], p[j], vb[2], vb[3]);
                 }
@@ -425,56 +465,65 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     cp_async_wait<0>();
 }
 
-// Joins the parts of the items that several CTAs worked on: one CTA per (CTA in which an item begins, row), each warp a share of the
-// parts, a lane HD / 32 columns.
-template <typename T, int HD>
+// Joins the parts of the items that several CTAs worked on.  blockIdx.x: the CTA in which an item begins; blockIdx.y: ROWS of its
+// rows, 4 / ROWS warps to a row, each warp a share of the parts, a lane HD / 32 columns.
+template <typename T, int HD, int ROWS>
 __global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedArgs a, int MT) {
     grid_launch_dependents();
     grid_dependency_wait();
-    constexpr int E = HD / 32;
+    constexpr int E = HD / 32, WPR = 4 / ROWS;
     __shared__ float so[4][HD];
     __shared__ float2 sml[4];
     const int4 d = a.desc[blockIdx.x];
     if (d.z == 0) return;
-    const int R = a.T * a.group, RT = (R + MT - 1) / MT;
-    const int head = d.y / RT, row0 = (d.y - head * RT) * MT, r = blockIdx.y;
-    if (row0 + r >= R) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int R = a.T * a.group, RT = (R + MT - 1) / MT;
+    const int head = d.y / RT, row0 = (d.y - head * RT) * MT, r = blockIdx.y * ROWS + warp / WPR;
+    const bool real = r < MT && row0 + r < R;
     float m = -INFINITY, l = 0.f, o[E] = {};
-    for (int f = warp; f < d.z; f += 4) {
-        const int64_t slot = f == 0 ? (int64_t)blockIdx.x * 2 + 1 : (int64_t)(blockIdx.x + f) * 2;
-        const float2 p = a.partial_ml[slot * MT + r];
-        float x[E];
+    if (real) {
+#pragma unroll 4
+        for (int f = warp % WPR; f < d.z; f += WPR) {
+            const int64_t slot = f == 0 ? (int64_t)blockIdx.x * 2 + 1 : (int64_t)(blockIdx.x + f) * 2;
+            const float2 p = a.partial_ml[slot * MT + r];
+            float x[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = a.partial[(slot * MT + r) * HD + lane * E + e];
-        const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
-        const float fo = ex2_approx(m - base), fn = ex2_approx(p.x - base);
-        m = top;
-        l = l * fo + p.y * fn;
+            for (int e = 0; e < E; ++e) x[e] = a.partial[(slot * MT + r) * HD + lane * E + e];
+            const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
+            const float fo = ex2_approx(m - base), fn = ex2_approx(p.x - base);
+            m = top;
+            l = l * fo + p.y * fn;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * fo + x[e] * fn;
+            for (int e = 0; e < E; ++e) o[e] = o[e] * fo + x[e] * fn;
+        }
     }
+    if (WPR > 1) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) so[warp][lane * E + e] = o[e];
-    if (lane == 0) sml[warp] = make_float2(m, l);
-    __syncthreads();
-    if (threadIdx.x >= HD / 8) return;
-    float top = -INFINITY, total = 0.f, x[8] = {};
+        for (int e = 0; e < E; ++e) so[warp][lane * E + e] = o[e];
+        if (lane == 0) sml[warp] = make_float2(m, l);
+        __syncthreads();
+        if (warp != 0) return;
+        m = -INFINITY;
+        l = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, sml[w].x);
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, sml[w].x);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float f = top == -INFINITY ? 1.f : ex2_approx(sml[w].x - top);
-        total += sml[w].y * f;
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += so[w][threadIdx.x * 8 + e] * f;
+        for (int w = 0; w < 4; ++w) {
+            const float f = m == -INFINITY ? 1.f : ex2_approx(sml[w].x - m);
+            l += sml[w].y * f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] += so[w][lane * E + e] * f;
+        }
     }
-    const float inv = 1.f / total;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    if (!real) return;
+    const float inv = 1.f / l;
     const int rr = row0 + r, t = rr / a.group, gq = rr - t * a.group;
-    reinterpret_cast<uint4*>((T*)a.out + d.x * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h)[threadIdx.x] = pack8<T>(x);
-    if (threadIdx.x == 0 && a.lse) a.lse[((int64_t)d.x * a.T + t) * a.nq + head * a.group + gq] = (top + log2f(total)) * 0.69314718055994531f;
+    T* out = (T*)a.out + d.x * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<typename Pack2<T>::type*>(out + e) = Pack2<T>::down(o[e] * inv, o[e + 1] * inv);
+    if (lane == 0 && a.lse) a.lse[((int64_t)d.x * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(l)) * 0.69314718055994531f;
 }
 
 }  // namespace jot
