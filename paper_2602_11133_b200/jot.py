@@ -495,29 +495,41 @@ _ELEMENTS = {torch.bfloat16: 0, torch.float16: 1}     # JOT_BF16, JOT_FP16
 STATUS_BAD_INDEX = 6                                    # what a status word becomes: a slot, page or length outside the pages
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _launch(device, where: str, fn, *args) -> None:
     """fn(*args, stream) on the current stream of the tensors' own device, whichever device is current."""
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+    index = device.index
+    if index == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status != 0:
+        raise JotError(status, where)
 
 
-def _int_ptr(t: Optional[torch.Tensor], name: str, device, shape) -> Optional[int]:
+def _int_ptr(t: Optional[torch.Tensor], name: str, device, n: int) -> Optional[int]:
+    """Pointer of an int32 tensor [n] on the device (None for None)."""
     if t is None:
         return None
     if t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
         raise TypeError(f"{name}: expected a contiguous int32 tensor on {device}, got {t.dtype} on {t.device}")
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dim() != 1 or t.numel() != n:
+        raise ValueError(f"{name}: expected shape ({n},), got {tuple(t.shape)}")
     return t.data_ptr()
 
 
-def _element_tensor(t: torch.Tensor, name: str, dtype, device, dims: int) -> None:
-    if not t.is_cuda or t.device != device or t.dtype != dtype or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise TypeError(f"{name}: expected a {dims}-D {dtype} tensor on {device} whose last dimension is contiguous, got "
-                        f"{t.dim()}-D {t.dtype} on {t.device} with strides {t.stride()}")
+def _element_strides(t: torch.Tensor, name: str, dtype, device, shape):
+    """Strides of a tensor of the given shape, element type and device whose last dimension is contiguous."""
+    strides = t.stride()
+    if t.dtype != dtype or t.device != device or len(strides) != len(shape) or (strides[-1] != 1 and shape[-1] > 1):
+        raise TypeError(f"{name}: expected a {len(shape)}-D {dtype} tensor on {device} whose last dimension is contiguous, got "
+                        f"{t.dim()}-D {t.dtype} on {t.device} with strides {strides}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return strides
 
 
 class KVPages:
@@ -525,19 +537,23 @@ class KVPages:
     (its last three dimensions) is contiguous; layers and pages may lie at any stride that is a multiple of 8 elements, so
     that k and v may be two halves of one tensor.  The tensors are borrowed and written in place."""
 
+    __slots__ = ("k", "v", "device", "dtype", "n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim", "_c", "_ref")
+
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
-        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _ELEMENTS or not k.is_cuda or k.device != v.device:
+        shape, ks, vs, device, dtype = k.shape, k.stride(), v.stride(), k.device, k.dtype
+        if len(shape) != 5 or v.shape != shape or v.dtype != dtype or dtype not in _ELEMENTS or device.type != "cuda" or v.device != device:
             raise TypeError("KVPages: k and v must be CUDA tensors [n_layers, n_pages, n_kv_heads, page_size, head_dim] of one "
                             "shape and device, bf16 or fp16")
-        n_layers, n_pages, n_kv_heads, page_size, head_dim = k.shape
-        for t in (k, v):
-            if not (t.numel() == 0 or t[0, 0].is_contiguous()):
+        n_layers, n_pages, n_kv_heads, page_size, head_dim = shape
+        inner = (page_size * head_dim, head_dim, 1)
+        for st in (ks, vs):
+            if st[2:] != inner and any(n > 1 and x != y for n, x, y in zip(shape[2:], st[2:], inner)):
                 raise TypeError("KVPages: the last three dimensions must be contiguous")
-        self.k, self.v = k, v
-        self.device, self.dtype = k.device, k.dtype
-        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
-        self._c = _KVPages(k.data_ptr(), v.data_ptr(), k.stride(0), v.stride(0), k.stride(1), v.stride(1), n_layers, n_pages,
-                           n_kv_heads, page_size, head_dim, _ELEMENTS[k.dtype])
+        self.k, self.v, self.device, self.dtype = k, v, device, dtype
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
+        self._c = _KVPages(k.data_ptr(), v.data_ptr(), ks[0], vs[0], ks[1], vs[1], n_layers, n_pages, n_kv_heads, page_size, head_dim,
+                           _ELEMENTS[dtype])
+        self._ref = C.byref(self._c)
 
     @staticmethod
     def empty(n_layers: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype=torch.bfloat16,
@@ -574,21 +590,14 @@ def rope_frequencies(rotary_dim: int, theta: float, factor: float = 1.0, origina
     return (f * (keep + (1.0 - keep) / factor)).to(torch.float32).to(device)
 
 
-def _heads(x: torch.Tensor, out: Optional[torch.Tensor], gain: Optional[torch.Tensor], name: str, device, dtype, rows, hd) -> _Heads:
-    _element_tensor(x, name, dtype, device, 3)
-    if x.shape[0] != rows or x.shape[2] != hd:
-        raise ValueError(f"{name}: expected [{rows}, heads, {hd}], got {tuple(x.shape)}")
-    h = _Heads(x.data_ptr(), x.stride(0), x.stride(1), None, 0, 0, None, x.shape[1])
-    if out is not None:
-        _element_tensor(out, name + "_out", dtype, device, 3)
-        if out.shape != x.shape:
-            raise ValueError(f"{name}_out: expected shape {tuple(x.shape)}, got {tuple(out.shape)}")
-        h.out, h.out_row_stride, h.out_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
-    if gain is not None:
-        if gain.dtype != dtype or gain.device != device or gain.shape != (hd,) or not gain.is_contiguous():
-            raise TypeError(f"{name}_gain: expected a contiguous {dtype} tensor [{hd}] on {device}")
-        h.gain = gain.data_ptr()
-    return h
+def _heads(x: torch.Tensor, out: Optional[torch.Tensor], gain: Optional[torch.Tensor], name: str, device, dtype, rows: int, hd: int) -> _Heads:
+    n = x.shape[1]
+    shape = (rows, n, hd)
+    xs = _element_strides(x, name, dtype, device, shape)
+    outs = (0, 0) if out is None else _element_strides(out, name + "_out", dtype, device, shape)
+    if gain is not None and (gain.dtype != dtype or gain.device != device or gain.dim() != 1 or gain.numel() != hd or not gain.is_contiguous()):
+        raise TypeError(f"{name}_gain: expected a contiguous {dtype} tensor [{hd}] on {device}")
+    return _Heads(x.data_ptr(), xs[0], xs[1], None if out is None else out.data_ptr(), outs[0], outs[1], None if gain is None else gain.data_ptr(), n)
 
 
 def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, rope: Rope,
@@ -601,29 +610,36 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.
     v go to `layer` of the pages at slots [rows] = page * page_size + offset (int32), and k_out is None.  A row with a
     negative position, and the pages of a row with a negative slot, stay as they were."""
     device, dtype = q.device, q.dtype
-    if dtype not in _ELEMENTS or q.dim() != 3:
-        raise TypeError(f"q: expected a 3-D bf16 or fp16 tensor, got {q.dim()}-D {dtype}")
+    if dtype not in _ELEMENTS or q.dim() != 3 or device.type != "cuda":
+        raise TypeError(f"q: expected a 3-D bf16 or fp16 CUDA tensor, got {q.dim()}-D {dtype} on {device}")
+    if k is not None and k.dim() != 3 or v is not None and v.dim() != 3:
+        raise TypeError("head_norm_rope: expected 3-D k and v")
     rows, _, hd = q.shape
     f = rope.inv_freq
     if f.dtype != torch.float32 or f.device != device or f.dim() != 1 or not f.is_contiguous():
         raise TypeError(f"rope.inv_freq: expected a contiguous 1-D float32 tensor on {device}")
-    if pages is not None and (k is None or v is None or slots is None or k_out is not None):
-        raise ValueError("head_norm_rope: pages need k, v and slots, and take the place of k_out")
-    if pages is None and (v is not None or slots is not None):
-        raise ValueError("head_norm_rope: v and slots go with pages")
-    if pages is not None and pages.device != device:
-        raise TypeError(f"pages: expected on {device}, got {pages.device}")
+    hk = hv = ref = None
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=dtype, device=device)
-    if k is not None and pages is None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=dtype, device=device)
-    hq = _heads(q, q_out, q_gain, "q", device, dtype, rows, hd)
-    hk = None if k is None else C.byref(_heads(k, k_out, k_gain, "k", device, dtype, rows, hd))
-    hv = None if v is None else C.byref(_heads(v, None, None, "v", device, dtype, rows, hd))
-    r = _Rope(f.data_ptr(), 2 * f.numel(), int(rope.interleaved), rope.magnitude)
-    _launch(device, "jot_head_norm_rope", _lib().jot_head_norm_rope, C.byref(hq), hk, C.byref(r), _ELEMENTS[dtype], rows, hd, eps,
-            _int_ptr(positions, "positions", device, (rows,)), hv, None if pages is None else C.byref(pages._c), layer,
-            _int_ptr(slots, "slots", device, (rows,)), _int_ptr(status, "status", device, (1,)))
+        q_out = torch.empty_like(q)
+    if pages is None:
+        if v is not None or slots is not None:
+            raise ValueError("head_norm_rope: v and slots go with pages")
+        if k is not None:
+            if k_out is None:
+                k_out = torch.empty_like(k)
+            hk = C.byref(_heads(k, k_out, k_gain, "k", device, dtype, rows, hd))
+    else:
+        if k is None or v is None or slots is None or k_out is not None:
+            raise ValueError("head_norm_rope: pages need k, v and slots, and take the place of k_out")
+        if pages.device != device:
+            raise TypeError(f"pages: expected on {device}, got {pages.device}")
+        ref = pages._ref
+        hk = C.byref(_heads(k, None, k_gain, "k", device, dtype, rows, hd))
+        hv = C.byref(_heads(v, None, None, "v", device, dtype, rows, hd))
+    _launch(device, "jot_head_norm_rope", _lib().jot_head_norm_rope, C.byref(_heads(q, q_out, q_gain, "q", device, dtype, rows, hd)), hk,
+            C.byref(_Rope(f.data_ptr(), 2 * f.numel(), rope.interleaved, rope.magnitude)), _ELEMENTS[dtype], rows, hd, eps,
+            _int_ptr(positions, "positions", device, rows), hv, ref, layer, _int_ptr(slots, "slots", device, rows),
+            _int_ptr(status, "status", device, 1))
     return q_out, k_out
 
 
@@ -631,14 +647,11 @@ def kv_write(pages: KVPages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tens
              status: Optional[torch.Tensor] = None) -> None:
     """Rows k, v [rows, n_kv_heads, head_dim] into `layer` of the pages at slots [rows] (int32; negative: skipped).  Slots must
     differ from each other."""
-    shape = (k.shape[0], pages.n_kv_heads, pages.head_dim)
-    for t, name in ((k, "k"), (v, "v")):
-        _element_tensor(t, name, pages.dtype, pages.device, 3)
-        if t.shape != shape:
-            raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
-    _launch(pages.device, "jot_kv_write", _lib().jot_kv_write, C.byref(pages._c), layer, k.shape[0], k.data_ptr(), k.stride(0),
-            k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), _int_ptr(slots, "slots", pages.device, (k.shape[0],)),
-            _int_ptr(status, "status", pages.device, (1,)))
+    device, rows = pages.device, k.shape[0]
+    shape = (rows, pages.n_kv_heads, pages.head_dim)
+    ks, vs = _element_strides(k, "k", pages.dtype, device, shape), _element_strides(v, "v", pages.dtype, device, shape)
+    _launch(device, "jot_kv_write", _lib().jot_kv_write, pages._ref, layer, rows, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+            _int_ptr(slots, "slots", device, rows), _int_ptr(status, "status", device, 1))
 
 
 def kv_copy_pages(pages: KVPages, src: Sequence[int], dst: Sequence[int]) -> None:
@@ -647,7 +660,7 @@ def kv_copy_pages(pages: KVPages, src: Sequence[int], dst: Sequence[int]) -> Non
         raise ValueError("kv_copy_pages: src and dst differ in length")
     n = len(src)
     pair = C.c_int32 * n
-    _launch(pages.device, "jot_kv_copy_pages", _lib().jot_kv_copy_pages, C.byref(pages._c), n, pair(*src), pair(*dst))
+    _launch(pages.device, "jot_kv_copy_pages", _lib().jot_kv_copy_pages, pages._ref, n, pair(*src), pair(*dst))
 
 
 @functools.lru_cache(maxsize=None)
@@ -665,28 +678,26 @@ def paged_attention(q: torch.Tensor, pages: KVPages, page_table: torch.Tensor, l
     gives zeros and -inf, a negative one leaves its sequence's rows of out and lse as they were.
 
     workspace: optional uint8 tensor of paged_attention_workspace_bytes(); calls that may overlap need one each."""
-    device = pages.device
-    _element_tensor(q, "q", pages.dtype, device, 4)
-    B, T, nq, hd = q.shape
-    if hd != pages.head_dim:
-        raise ValueError(f"q: expected heads of {pages.head_dim}, got {hd}")
+    device, shape = pages.device, q.shape
+    if len(shape) != 4 or shape[3] != pages.head_dim:
+        raise ValueError(f"q: expected [B, T, n_q_heads, {pages.head_dim}], got {tuple(shape)}")
+    B, T, nq, hd = shape
+    qs = _element_strides(q, "q", pages.dtype, device, shape)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=device)
-    else:
-        _element_tensor(out, "out", pages.dtype, device, 4)
-        if out.shape != q.shape:
-            raise ValueError(f"out: expected shape {tuple(q.shape)}, got {tuple(out.shape)}")
-    if lse is not None and (lse.dtype != torch.float32 or lse.device != device or lse.shape != q.shape[:3] or not lse.is_contiguous()):
-        raise TypeError(f"lse: expected a contiguous float32 tensor {tuple(q.shape[:3])} on {device}")
-    if page_table.dtype != torch.int32 or page_table.device != device or page_table.dim() != 2 or page_table.shape[0] != B or (
-            page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        out = torch.empty_like(q)
+    outs = _element_strides(out, "out", pages.dtype, device, shape)
+    if lse is not None and (lse.dtype != torch.float32 or lse.device != device or lse.shape != shape[:3] or not lse.is_contiguous()):
+        raise TypeError(f"lse: expected a contiguous float32 tensor {tuple(shape[:3])} on {device}")
+    table = page_table.shape
+    if page_table.dtype != torch.int32 or page_table.device != device or len(table) != 2 or table[0] != B or (
+            table[1] > 1 and page_table.stride(1) != 1):
         raise TypeError(f"page_table: expected an int32 tensor [{B}, max_pages] on {device} with contiguous rows")
     if workspace is None:
         workspace = torch.empty(paged_attention_workspace_bytes(T, nq, pages.n_kv_heads, hd), dtype=torch.uint8, device=device)
     elif workspace.dtype != torch.uint8 or workspace.device != device or not workspace.is_contiguous():
         raise TypeError(f"workspace: expected a contiguous uint8 tensor on {device}")
-    _launch(device, "jot_paged_attention", _lib().jot_paged_attention, q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), out.data_ptr(),
-            out.stride(0), out.stride(1), out.stride(2), None if lse is None else lse.data_ptr(), B, T, nq, C.byref(pages._c), layer,
-            page_table.data_ptr(), page_table.stride(0), page_table.shape[1], _int_ptr(lens, "lens", device, (B,)),
-            hd ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel(), _int_ptr(status, "status", device, (1,)))
+    _launch(device, "jot_paged_attention", _lib().jot_paged_attention, q.data_ptr(), qs[0], qs[1], qs[2], out.data_ptr(), outs[0], outs[1], outs[2],
+            None if lse is None else lse.data_ptr(), B, T, nq, pages._ref, layer, page_table.data_ptr(), page_table.stride(0), table[1],
+            _int_ptr(lens, "lens", device, B), hd ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel(),
+            _int_ptr(status, "status", device, 1))
     return out
