@@ -25,6 +25,8 @@ namespace jot {
 constexpr int32_t kStatusBadIndex = 6;     // a slot, a page or a length outside the pages: skipped or read as zeros
 
 template <typename T> struct Pack2;
+template <typename T> struct PackIsBf16 { static constexpr bool value = false; };
+template <> struct PackIsBf16<__nv_bfloat16> { static constexpr bool value = true; };
 template <> struct Pack2<__nv_bfloat16> {
     using type = __nv_bfloat162;
     static __device__ __forceinline__ float2 up(type v) { return __bfloat1622float2(v); }

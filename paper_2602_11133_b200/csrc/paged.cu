@@ -1,6 +1,7 @@
 // Entry points of decoding over a paged key-value cache: argument checks and launches (kernels: heads.cuh, kv_pages.cuh,
 // paged_attention.cuh).
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <memory>
@@ -10,6 +11,7 @@
 #include "host.cuh"
 #include "kv_pages.cuh"
 #include "paged_attention.cuh"
+#include "paged_attention_umma.cuh"
 
 using namespace jot;
 
@@ -96,19 +98,29 @@ int check_moves(int n_pages, int n, const int32_t* src, const int32_t* dst) {
     return JOT_OK;
 }
 
-// Rows an attention CTA works on: as few tiles of 16 as the rows of a key head need, up to four.
-int paged_row_tile(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
+// Rows an attention CTA works on: a warp's 16, the 128 of a tcgen05 tile, or two of those.
+int paged_row_tile(int rows) { return rows <= 16 ? 16 : (rows <= 128 ? 128 : 256); }
 
 struct PagedSpace {
     size_t desc, ml, partial, total;
 };
 PagedSpace paged_space(int row_tile, int head_dim) {
+    const size_t ctas = row_tile == 16 ? kPagedMaxCtas : kUmmaPagedMaxCtas;
     PagedSpace s;
     s.desc = 0;
-    s.ml = align_up((size_t)kPagedMaxCtas * sizeof(int4), 256);
-    s.partial = s.ml + align_up((size_t)kPagedMaxCtas * 2 * row_tile * sizeof(float2), 256);
-    s.total = s.partial + (size_t)kPagedMaxCtas * 2 * row_tile * head_dim * sizeof(float);
+    s.ml = align_up(ctas * sizeof(int4), 256);
+    s.partial = s.ml + align_up(ctas * 2 * row_tile * sizeof(float2), 256);
+    s.total = s.partial + ctas * 2 * row_tile * head_dim * sizeof(float);
     return s;
+}
+
+// The second kernel: four warps to a row where an item may be in many parts (few items on many CTAs), a warp to a row otherwise.
+template <typename T, int HD>
+int launch_join(const PagedArgs& a, int grid, int row_tile, cudaStream_t st) {
+    const int all = a.T * a.group, rows = std::min(row_tile, all), row_tiles = (all + row_tile - 1) / row_tile;
+    if (grid > 8ll * a.B * a.nkv * row_tiles) launch_k((paged_join_kernel<T, HD, 1>), dim3((unsigned)grid, (unsigned)rows), dim3(kPagedThreads), 0, st, a, row_tile);
+    else launch_k((paged_join_kernel<T, HD, 4>), dim3((unsigned)grid, (unsigned)((rows + 3) / 4)), dim3(kPagedThreads), 0, st, a, row_tile);
+    return launch_check();
 }
 
 template <typename T, int HD, int WM>
@@ -130,18 +142,41 @@ int launch_paged_t(const DeviceInfo* di, const PagedArgs& a, int64_t most_tiles,
     launch_k(kernel, dim3((unsigned)grid), dim3(kPagedThreads), smem, st, a);
     JOT_TRY(launch_check());
     if (one_tile) return JOT_OK;                                        // an item of one tile is never in two CTAs
-    // Four warps to a row where an item may be in many parts (few items on many CTAs), a warp to a row otherwise.
-    const int rows = std::min(16 * WM, a.T * a.group), row_tiles = (a.T * a.group + 16 * WM - 1) / (16 * WM);
-    if (grid > 8ll * a.B * a.nkv * row_tiles) launch_k((paged_join_kernel<T, HD, 1>), dim3((unsigned)grid, (unsigned)rows), dim3(kPagedThreads), 0, st, a, 16 * WM);
-    else launch_k((paged_join_kernel<T, HD, 4>), dim3((unsigned)grid, (unsigned)((rows + 3) / 4)), dim3(kPagedThreads), 0, st, a, 16 * WM);
-    return launch_check();
+    return launch_join<T, HD>(a, grid, 16 * WM, st);
+}
+
+template <typename T, int HD, int MODE>
+int launch_paged_umma(const DeviceInfo* di, const PagedArgs& a, int64_t most_tiles, bool one_tile, cudaStream_t st) {
+    static thread_local bool attr_set[64] = {};
+    int dev = 0;
+    JOT_CUDA(cudaGetDevice(&dev));
+    auto* kernel = paged_attention_umma_kernel<T, HD, MODE>;
+    constexpr int smem = UmmaPagedSmem<HD, MODE>::DYN_BYTES;
+    if (!attr_set[dev & 63]) {
+        JOT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        attr_set[dev & 63] = true;
+    }
+    const int grid = (int)std::min<int64_t>(std::max<int64_t>(most_tiles, 1), std::min(di->sms, kUmmaPagedMaxCtas));
+    launch_k(kernel, dim3((unsigned)grid), dim3(kUmmaPagedThreads), smem, st, a);
+    JOT_TRY(launch_check());
+    if (one_tile) return JOT_OK;
+    return launch_join<T, HD>(a, grid, MODE == PAGED_TWO ? 256 : 128, st);
 }
 
 template <typename T, int HD>
-int launch_paged(const DeviceInfo* di, const PagedArgs& a, int row_tile, int64_t most_tiles, bool one_tile, cudaStream_t st) {
-    if (row_tile == 16) return launch_paged_t<T, HD, 1>(di, a, most_tiles, one_tile, st);
-    if (row_tile == 32) return launch_paged_t<T, HD, 2>(di, a, most_tiles, one_tile, st);
-    return launch_paged_t<T, HD, 4>(di, a, most_tiles, one_tile, st);
+int launch_paged(const DeviceInfo* di, const PagedArgs& a, int row_tile, cudaStream_t st) {
+    // what the table can hold bounds the line of tiles
+    auto tiles_of = [&](int keys) { return ((int64_t)a.max_pages * a.pages.page_size + keys - 1) / keys; };
+    const int64_t items = (int64_t)a.nkv * ((a.T * a.group + row_tile - 1) / row_tile);
+    auto most = [&](int64_t tiles) {
+        int64_t n = std::min<int64_t>(items, kPagedMaxCtas) * std::min(a.B, kPagedMaxCtas);
+        return std::min<int64_t>(kPagedMaxCtas, n) * std::min<int64_t>(tiles, kPagedMaxCtas);
+    };
+    const int64_t small = tiles_of(kPagedTile), large = tiles_of(kUmmaPagedTile);
+    if (row_tile == 16) return launch_paged_t<T, HD, 1>(di, a, most(small), small <= 1, st);
+    if (row_tile == 256) return launch_paged_umma<T, HD, PAGED_TWO>(di, a, most(large), large <= 1, st);
+    if (a.T * a.group <= 32) return launch_paged_umma<T, HD, PAGED_SMALL>(di, a, most(large), large <= 1, st);
+    return launch_paged_umma<T, HD, PAGED_ONE>(di, a, most(large), large <= 1, st);
 }
 
 }  // namespace
@@ -259,7 +294,7 @@ int jot_paged_attention(const void* d_q, int64_t q_seq_stride, int64_t q_row_str
     if (!d_workspace || !aligned16(d_workspace) || workspace_bytes < sp.total) return JOT_ERR_WORKSPACE;
     const int64_t row_tiles = (rows + row_tile - 1) / row_tile, items = row_tiles * pages->n_kv_heads;
     const int64_t most_keys = (int64_t)max_pages * pages->page_size;
-    if (items > INT32_MAX || most_keys > INT32_MAX - kPagedTile) return JOT_ERR_SHAPE;
+    if (items > INT32_MAX || most_keys > INT32_MAX - kUmmaPagedTile) return JOT_ERR_SHAPE;
     DeviceInfo* di = nullptr;
     JOT_TRY(device_info(&di));
     PagedArgs a{};
@@ -269,19 +304,15 @@ int jot_paged_attention(const void* d_q, int64_t q_seq_stride, int64_t q_row_str
     a.B = B; a.T = T; a.nq = n_q_heads; a.nkv = pages->n_kv_heads; a.group = group;
     a.pages = layer_pages(pages, layer);
     a.table = d_page_table; a.table_stride = table_stride; a.max_pages = max_pages; a.lens = d_lens;
-    a.scale_log2 = scale * 1.4426950408889634f;
+    // (a scale of zero as the smallest normal number: every score is zero all the same, and a key that is not there stays at minus infinity)
+    a.scale_log2 = scale == 0.f ? FLT_MIN : scale * 1.4426950408889634f;
     uint8_t* ws = (uint8_t*)d_workspace;
     a.desc = (int4*)(ws + sp.desc); a.partial_ml = (float2*)(ws + sp.ml); a.partial = (float*)(ws + sp.partial);
     a.status = d_status;
-    // what the table can hold bounds the line of tiles
-    const int64_t tiles = (most_keys + kPagedTile - 1) / kPagedTile;
-    const int64_t most_tiles = tiles > kPagedMaxCtas ? kPagedMaxCtas : std::min<int64_t>(kPagedMaxCtas, std::min<int64_t>(items, kPagedMaxCtas) * tiles * std::min(B, kPagedMaxCtas));
     cudaStream_t st = (cudaStream_t)stream;
     if (pages->dtype == JOT_BF16)
-        return hd == 128 ? launch_paged<__nv_bfloat16, 128>(di, a, row_tile, most_tiles, tiles <= 1, st)
-                         : launch_paged<__nv_bfloat16, 64>(di, a, row_tile, most_tiles, tiles <= 1, st);
-    return hd == 128 ? launch_paged<__half, 128>(di, a, row_tile, most_tiles, tiles <= 1, st)
-                     : launch_paged<__half, 64>(di, a, row_tile, most_tiles, tiles <= 1, st);
+        return hd == 128 ? launch_paged<__nv_bfloat16, 128>(di, a, row_tile, st) : launch_paged<__nv_bfloat16, 64>(di, a, row_tile, st);
+    return hd == 128 ? launch_paged<__half, 128>(di, a, row_tile, st) : launch_paged<__half, 64>(di, a, row_tile, st);
 }
 
 }  // extern "C"

@@ -76,6 +76,10 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool r
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// one arrival on the barrier once all requests this thread has made so far have landed
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -98,6 +102,80 @@ __host__ __device__ __forceinline__ int64_t paged_share(int64_t total, int ctas,
 // the CTA that has tile t
 __host__ __device__ __forceinline__ int paged_owner(int64_t total, int ctas, int64_t t) { return (int)(((t + 1) * ctas - 1) / total); }
 
+struct PagedRangeSmem {
+    int64_t warp_tot[16], in_seq;
+    int b;
+};
+
+// The share of this CTA on the line of tiles of `tile` keys, per_b items a sequence; sequences without a key are answered here:
+// zeros, and the logarithm of nothing.  All THREADS threads of the CTA call it; lens is read after the preceding kernel's end.
+template <typename T, int HD, int THREADS>
+__device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, int per_b, PagedRangeSmem& sm) {
+    constexpr int WARPS = THREADS / 32, CPR = HD / 8;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    auto tiles_of = [&](int b) -> int64_t {
+        const int n = b < a.B ? paged_len(a, b) : 0;
+        return n > 0 ? (int64_t)((n + tile - 1) / tile) * per_b : 0;
+    };
+    auto totals = [&]() {
+        int64_t t = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) t += sm.warp_tot[w];
+        return t;
+    };
+    PagedRange rg;
+    int64_t sum = 0;
+    for (int b = tid; b < a.B; b += THREADS) {
+        sum += tiles_of(b);
+        if (blockIdx.x == 0 && a.status && a.lens[b] > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) sm.warp_tot[warp] = sum;
+    __syncthreads();
+    rg.total = totals();
+    rg.ctas = (int)min((int64_t)gridDim.x, rg.total);
+    rg.begin = rg.end = rg.in_seq = 0;
+    rg.b = 0;
+    if ((int)blockIdx.x < rg.ctas) {
+        rg.begin = paged_share(rg.total, rg.ctas, blockIdx.x);
+        rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
+        int64_t before = 0;
+        for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+            const int64_t mine = tiles_of(b0 + tid);
+            int64_t inc = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += up;
+            }
+            __syncthreads();                                        // warp_tot is read by everyone before it is written again
+            if (lane == 31) sm.warp_tot[warp] = inc;
+            __syncthreads();
+            int64_t start = before + inc - mine;
+            for (int w = 0; w < warp; ++w) start += sm.warp_tot[w];
+            if (start <= rg.begin && rg.begin < start + mine) {
+                sm.b = b0 + tid;
+                sm.in_seq = rg.begin - start;
+            }
+            before += totals();
+            if (before > rg.begin) break;
+        }
+        __syncthreads();
+        rg.b = sm.b;
+        rg.in_seq = sm.in_seq;
+    }
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+        if (a.lens[b] != 0 && !(a.lens[b] > 0 && a.max_pages == 0)) continue;
+        for (int i = tid; i < a.T * a.nq * CPR; i += THREADS) {
+            const int row = i / CPR, t = row / a.nq, h = row - t * a.nq;
+            reinterpret_cast<uint4*>((T*)a.out + b * a.o_b + t * a.o_t + h * a.o_h)[i % CPR] = make_uint4(0, 0, 0, 0);
+            if (i % CPR == 0 && a.lse) a.lse[(int64_t)b * a.T * a.nq + row] = -INFINITY;
+        }
+    }
+    return rg;
+}
+
 template <int HD>
 struct PagedSmem {
     static constexpr int TILE_BYTES = kPagedTile * HD * 2;                       // K or V of one stage
@@ -116,9 +194,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     float* merge = reinterpret_cast<float*>(smem + kPagedStages * SM::STAGE_BYTES);
     __shared__ float2 ml[WK][MT];
     __shared__ uint64_t row_at[2][2 * kPagedTile];                      // addresses of a tile's key rows, then of its value rows
-    __shared__ int64_t warp_tot[4];
-    __shared__ int found_b;
-    __shared__ int64_t found_in_seq;
+    __shared__ PagedRangeSmem range_smem;
 
     grid_launch_dependents();
     grid_dependency_wait();
@@ -126,63 +202,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     const int R = a.T * a.group, RT = (R + MT - 1) / MT;
     const int per_b = a.nkv * RT;                                       // items of a sequence
 
-    // ---- the line of tiles and this CTA's share ----
-    auto tiles_of = [&](int b) -> int64_t {
-        const int n = b < a.B ? paged_len(a, b) : 0;
-        return n > 0 ? (int64_t)((n + kPagedTile - 1) / kPagedTile) * per_b : 0;
-    };
-    PagedRange rg;
-    {
-        int64_t sum = 0;
-        for (int b = tid; b < a.B; b += kPagedThreads) {
-            sum += tiles_of(b);
-            if (blockIdx.x == 0 && a.status && a.lens[b] > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) warp_tot[warp] = sum;
-        __syncthreads();
-        rg.total = warp_tot[0] + warp_tot[1] + warp_tot[2] + warp_tot[3];
-        rg.ctas = (int)min((int64_t)gridDim.x, rg.total);
-        rg.begin = rg.end = 0;
-        if ((int)blockIdx.x < rg.ctas) {
-            rg.begin = paged_share(rg.total, rg.ctas, blockIdx.x);
-            rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
-            int64_t before = 0;
-            for (int b0 = 0; b0 < a.B; b0 += kPagedThreads) {
-                const int64_t mine = tiles_of(b0 + tid);
-                int64_t inc = mine;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
-                    if (lane >= o) inc += up;
-                }
-                __syncthreads();                                        // warp_tot is read by everyone before it is written again
-                if (lane == 31) warp_tot[warp] = inc;
-                __syncthreads();
-                int64_t start = before + inc - mine;
-                for (int w = 0; w < warp; ++w) start += warp_tot[w];
-                if (start <= rg.begin && rg.begin < start + mine) {
-                    found_b = b0 + tid;
-                    found_in_seq = rg.begin - start;
-                }
-                before += warp_tot[0] + warp_tot[1] + warp_tot[2] + warp_tot[3];
-                if (before > rg.begin) break;
-            }
-            __syncthreads();
-            rg.b = found_b;
-            rg.in_seq = found_in_seq;
-        }
-    }
-    // sequences without a key: zeros, and the logarithm of nothing
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-        if (a.lens[b] != 0 && !(a.lens[b] > 0 && a.max_pages == 0)) continue;
-        for (int i = tid; i < a.T * a.nq * CPR; i += kPagedThreads) {
-            const int row = i / CPR, t = row / a.nq, h = row - t * a.nq;
-            reinterpret_cast<uint4*>((T*)a.out + b * a.o_b + t * a.o_t + h * a.o_h)[i % CPR] = make_uint4(0, 0, 0, 0);
-            if (i % CPR == 0 && a.lse) a.lse[(int64_t)b * a.T * a.nq + row] = -INFINITY;
-        }
-    }
+    const PagedRange rg = paged_range<T, HD, kPagedThreads>(a, kPagedTile, per_b, range_smem);
     if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if ((int)blockIdx.x >= rg.ctas) return;
 
