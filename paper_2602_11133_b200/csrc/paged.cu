@@ -98,8 +98,8 @@ int check_moves(int n_pages, int n, const int32_t* src, const int32_t* dst) {
     return JOT_OK;
 }
 
-// Rows an attention CTA works on: a warp's 16, the 128 of a tcgen05 tile, or two of those.
-int paged_row_tile(int rows) { return rows <= 16 ? 16 : (rows <= 128 ? 128 : 256); }
+// Rows an attention CTA works on: a warp's 16; a tcgen05 tile of 128 that holds them four times, twice or once; two such tiles.
+int paged_row_tile(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : (rows <= 128 ? 128 : 256))); }
 
 struct PagedSpace {
     size_t desc, ml, partial, total;
@@ -123,8 +123,15 @@ int launch_join(const PagedArgs& a, int grid, int row_tile, cudaStream_t st) {
     return launch_check();
 }
 
+// What the table can hold bounds the line of tiles: of an item, and of them all (no more than there may be CTAs).
+int64_t paged_tiles(const PagedArgs& a, int keys) { return ((int64_t)a.max_pages * a.pages.page_size + keys - 1) / keys; }
+int64_t paged_most(const PagedArgs& a, int64_t items, int64_t tiles) {
+    const int64_t n = std::min<int64_t>(items, kPagedMaxCtas) * std::min(a.B, kPagedMaxCtas);
+    return std::max<int64_t>(1, std::min<int64_t>(kPagedMaxCtas, n) * std::min<int64_t>(tiles, kPagedMaxCtas));
+}
+
 template <typename T, int HD, int WM>
-int launch_paged_t(const DeviceInfo* di, const PagedArgs& a, int64_t most_tiles, bool one_tile, cudaStream_t st) {
+int launch_paged_t(const DeviceInfo* di, const PagedArgs& a, int64_t items, cudaStream_t st) {
     static thread_local int per_sm[64] = {};
     int dev = 0;
     JOT_CUDA(cudaGetDevice(&dev));
@@ -138,45 +145,72 @@ int launch_paged_t(const DeviceInfo* di, const PagedArgs& a, int64_t most_tiles,
         if (n < 1) return JOT_ERR_DEVICE;
         occ = n;
     }
-    const int grid = (int)std::min<int64_t>(std::max<int64_t>(most_tiles, 1), std::min(occ * di->sms, kPagedMaxCtas));
+    const int64_t tiles = paged_tiles(a, kPagedTile);
+    const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(occ * di->sms, kPagedMaxCtas));
     launch_k(kernel, dim3((unsigned)grid), dim3(kPagedThreads), smem, st, a);
     JOT_TRY(launch_check());
-    if (one_tile) return JOT_OK;                                        // an item of one tile is never in two CTAs
-    return launch_join<T, HD>(a, grid, 16 * WM, st);
+    return tiles <= 1 ? JOT_OK : launch_join<T, HD>(a, grid, 16 * WM, st);     // an item of one tile is never in two CTAs
 }
 
-template <typename T, int HD, int MODE>
-int launch_paged_umma(const DeviceInfo* di, const PagedArgs& a, int64_t most_tiles, bool one_tile, cudaStream_t st) {
+// (head_dim, key of the page, head, page); a box is 64 columns of a page's keys, or of 128 of them.  Out-of-range pages read as zeros.
+int make_map_pages(const DeviceInfo* di, CUtensorMap* map, const PagedArgs& a, const void* ptr, int64_t page_stride, int hd, int dtype) {
+    const cuuint64_t head_bytes = (cuuint64_t)a.pages.page_size * hd * 2;
+    cuuint64_t dims[4] = {(cuuint64_t)hd, (cuuint64_t)a.pages.page_size, (cuuint64_t)a.nkv, (cuuint64_t)a.pages.n_pages};
+    cuuint64_t strides[3] = {(cuuint64_t)hd * 2, head_bytes, a.pages.n_pages > 1 ? (cuuint64_t)page_stride * 2 : head_bytes * a.nkv};
+    cuuint32_t box[4] = {64, (cuuint32_t)std::min(a.pages.page_size, 128), 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    CUresult r = di->encode(map, dtype == JOT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(ptr), dims, strides,
+                            box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        g_last_cuda_error = (int)cudaErrorInvalidValue;
+        return JOT_ERR_CUDA;
+    }
+    return JOT_OK;
+}
+
+template <typename T, int HD, int ROWS, bool TMA>
+int launch_paged_umma_t(const DeviceInfo* di, const PagedArgs& a, int grid, cudaStream_t st) {
     static thread_local bool attr_set[64] = {};
     int dev = 0;
     JOT_CUDA(cudaGetDevice(&dev));
-    auto* kernel = paged_attention_umma_kernel<T, HD, MODE>;
-    constexpr int smem = UmmaPagedSmem<HD, MODE>::DYN_BYTES;
+    auto* kernel = paged_attention_umma_kernel<T, HD, ROWS, TMA>;
+    constexpr int smem = UmmaPagedSmem<HD>::DYN_BYTES;
     if (!attr_set[dev & 63]) {
         JOT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         attr_set[dev & 63] = true;
     }
-    const int grid = (int)std::min<int64_t>(std::max<int64_t>(most_tiles, 1), std::min(di->sms, kUmmaPagedMaxCtas));
-    launch_k(kernel, dim3((unsigned)grid), dim3(kUmmaPagedThreads), smem, st, a);
-    JOT_TRY(launch_check());
-    if (one_tile) return JOT_OK;
-    return launch_join<T, HD>(a, grid, MODE == PAGED_TWO ? 256 : 128, st);
+    CUtensorMap mk, mv;
+    if (TMA) {
+        const int dtype = PackIsBf16<T>::value ? JOT_BF16 : JOT_FP16;
+        JOT_TRY(make_map_pages(di, &mk, a, a.pages.k, a.pages.k_page, HD, dtype));
+        JOT_TRY(make_map_pages(di, &mv, a, a.pages.v, a.pages.v_page, HD, dtype));
+    } else {
+        std::memset(&mk, 0, sizeof(mk));
+        mv = mk;
+    }
+    launch_k(kernel, dim3((unsigned)grid), dim3(UmmaPagedRoles<TMA>::THREADS), smem, st, a, mk, mv);
+    return launch_check();
+}
+
+template <typename T, int HD, int ROWS>
+int launch_paged_umma(const DeviceInfo* di, const PagedArgs& a, int64_t items, cudaStream_t st) {
+    const bool tma = paged_tma_pages(a.pages.page_size) && a.pages.k_page >= 0 && a.pages.v_page >= 0;
+    const int64_t tiles = paged_tiles(a, tma ? paged_tma_keys(a.pages.page_size) : kUmmaPagedTile);
+    const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(di->sms, kUmmaPagedMaxCtas));
+    if (tma) JOT_TRY((launch_paged_umma_t<T, HD, ROWS, true>(di, a, grid, st)));
+    else JOT_TRY((launch_paged_umma_t<T, HD, ROWS, false>(di, a, grid, st)));
+    return tiles <= 1 ? JOT_OK : launch_join<T, HD>(a, grid, ROWS, st);
 }
 
 template <typename T, int HD>
 int launch_paged(const DeviceInfo* di, const PagedArgs& a, int row_tile, cudaStream_t st) {
-    // what the table can hold bounds the line of tiles
-    auto tiles_of = [&](int keys) { return ((int64_t)a.max_pages * a.pages.page_size + keys - 1) / keys; };
-    const int64_t items = (int64_t)a.nkv * ((a.T * a.group + row_tile - 1) / row_tile);
-    auto most = [&](int64_t tiles) {
-        int64_t n = std::min<int64_t>(items, kPagedMaxCtas) * std::min(a.B, kPagedMaxCtas);
-        return std::min<int64_t>(kPagedMaxCtas, n) * std::min<int64_t>(tiles, kPagedMaxCtas);
-    };
-    const int64_t small = tiles_of(kPagedTile), large = tiles_of(kUmmaPagedTile);
-    if (row_tile == 16) return launch_paged_t<T, HD, 1>(di, a, most(small), small <= 1, st);
-    if (row_tile == 256) return launch_paged_umma<T, HD, PAGED_TWO>(di, a, most(large), large <= 1, st);
-    if (a.T * a.group <= 32) return launch_paged_umma<T, HD, PAGED_SMALL>(di, a, most(large), large <= 1, st);
-    return launch_paged_umma<T, HD, PAGED_ONE>(di, a, most(large), large <= 1, st);
+    const int rows = a.T * a.group;
+    const int64_t items = (int64_t)a.nkv * ((rows + row_tile - 1) / row_tile);
+    if (row_tile == 16) return launch_paged_t<T, HD, 1>(di, a, items, st);
+    if (row_tile == 32) return launch_paged_umma<T, HD, 32>(di, a, items, st);
+    if (row_tile == 64) return launch_paged_umma<T, HD, 64>(di, a, items, st);
+    return row_tile == 128 ? launch_paged_umma<T, HD, 128>(di, a, items, st) : launch_paged_umma<T, HD, 256>(di, a, items, st);
 }
 
 }  // namespace

@@ -124,15 +124,19 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
         return t;
     };
     PagedRange rg;
-    int64_t sum = 0;
+    const int64_t first = tiles_of(tid);
+    int64_t sum = first;
+    bool empty = false;
     for (int b = tid; b < a.B; b += THREADS) {
-        sum += tiles_of(b);
-        if (blockIdx.x == 0 && a.status && a.lens[b] > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
+        if (b != tid) sum += tiles_of(b);
+        const int n = a.lens[b];
+        empty |= paged_len(a, b) == 0;
+        if (blockIdx.x == 0 && a.status && n > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) sm.warp_tot[warp] = sum;
-    __syncthreads();
+    empty = __syncthreads_or(empty);
     rg.total = totals();
     rg.ctas = (int)min((int64_t)gridDim.x, rg.total);
     rg.begin = rg.end = rg.in_seq = 0;
@@ -142,7 +146,7 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
         rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
         int64_t before = 0;
         for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-            const int64_t mine = tiles_of(b0 + tid);
+            const int64_t mine = b0 == 0 ? first : tiles_of(b0 + tid);
             int64_t inc = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -153,7 +157,8 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
             if (lane == 31) sm.warp_tot[warp] = inc;
             __syncthreads();
             int64_t start = before + inc - mine;
-            for (int w = 0; w < warp; ++w) start += sm.warp_tot[w];
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) start += w < warp ? sm.warp_tot[w] : 0;
             if (start <= rg.begin && rg.begin < start + mine) {
                 sm.b = b0 + tid;
                 sm.in_seq = rg.begin - start;
@@ -165,8 +170,8 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
         rg.b = sm.b;
         rg.in_seq = sm.in_seq;
     }
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-        if (a.lens[b] != 0 && !(a.lens[b] > 0 && a.max_pages == 0)) continue;
+    for (int b = blockIdx.x; empty && b < a.B; b += gridDim.x) {
+        if (paged_len(a, b) != 0) continue;
         for (int i = tid; i < a.T * a.nq * CPR; i += THREADS) {
             const int row = i / CPR, t = row / a.nq, h = row - t * a.nq;
             reinterpret_cast<uint4*>((T*)a.out + b * a.o_b + t * a.o_t + h * a.o_h)[i % CPR] = make_uint4(0, 0, 0, 0);

@@ -5,38 +5,54 @@
 //   pages: the head dimension runs along 128-byte rows (16-byte chunk c of row r at c ^ (r mod 8)), which is the first product's
 //   K-major operand for Q and K, and for V the second product's MN-major one, so nothing is transposed.
 //
-// Two streams of work share the tensor pipe, each with a score buffer, an accumulator and a warpgroup of its own (thread = row):
-// while one stream's rows are in exponentials, the other's products run.
-//   TWO    more than 128 rows: the streams are two tiles of 128 rows over the same keys
-//   !TWO   at most 128 rows: the streams are the even and the odd tiles of keys over the same rows, and meet at the end
+// Two streams of work share the tensor pipe, each with a score buffer, an accumulator, a warpgroup (thread = row) and a warp that
+// issues its products: while one stream's rows are in exponentials, the other's products run.  ROWS = 256: the streams are two tiles
+// of 128 rows over the same keys.  ROWS <= 128: they are the even and the odd tiles of keys over the same rows, and meet at the end.
+// With at most 64 or 32 rows the tile of 128 holds them twice or four times over, and each copy's threads take their share of a tile's keys
+// (the probabilities of the others are zeros): what a thread has to do for a tile, which is what few rows wait for, is a half or
+// a quarter, and the copies meet at the end as the streams do.
 // The reference maximum of a row follows a tile's maximum only when that exceeds it by more than 2^8 (probabilities up to 256
 // are as exact as those up to 1); then the row of the accumulator is rescaled in tensor memory.
 //
-// The keys come by cp.async, 16 bytes a request, since pages may be of any size; four producer warps look up page entries two tiles
-// ahead, leave row addresses one tile ahead, and never wait for a request: each arrives on its stage's barrier when it has landed.
+// Pages of a multiple of 8 keys come by TMA (one box per page and 64 columns; a tile is as many whole pages as fit into 128 rows, or
+// 128 keys of a larger page), others by cp.async, 16 bytes a request, which costs four warps and the rate at which an SM takes
+// such requests.
 //
-//   warps 0-3, 4-7  softmax of stream 0 and 1      warps 8-11  producers      warp 12  MMA issuer
+//   warps 0-3, 4-7   softmax of stream 0 and 1
+//   by TMA           warp 8 keys and values, warps 9, 10 products, warp 11 queries
+//   by cp.async      warps 8-11 keys, values and queries (page entries two tiles ahead, row addresses one), warps 12, 13 products
 #pragma once
 #include "paged_attention.cuh"
 
 namespace jot {
 
-constexpr int kUmmaPagedThreads = 416;
-constexpr int kUmmaPagedTile = 128;
-constexpr int kUmmaPagedMaxCtas = 160;      // one per SM
+constexpr int kUmmaPagedTile = 128;        // rows of a tile of keys in shared memory
+constexpr int kUmmaPagedMaxCtas = 160;     // one per SM
 
-enum { PAGED_SMALL = 0, PAGED_ONE = 1, PAGED_TWO = 2 };      // at most 32 rows of a key head, at most 128, more
-
-template <int HD, int MODE>
+template <int HD>
 struct UmmaPagedSmem {
     static constexpr int TILE_BYTES = 128 * HD * 2;               // 128 rows: a tile of Q, K or V
-    // Two tiles of queries (the streams', or this part's and the next one's), then the stages of keys and values.  Up to 32 rows the
-    // queries take the room of 32 (the products read on into what follows: rows that nobody looks at), which leaves a third stage.
-    static constexpr int Q_ROWS = MODE == PAGED_SMALL ? 32 : 128;
-    static constexpr int Q_BYTES = Q_ROWS * HD * 2;
-    static constexpr int STAGES = MODE == PAGED_SMALL ? 3 : 2;
-    static constexpr int DYN_BYTES = 2 * Q_BYTES + 2 * STAGES * TILE_BYTES + 1024;
+    // Of K and of V.  With ROWS <= 128 each stream has half of them to itself: nobody waits on a barrier whose phases it does not see one by
+    // one, so a parity says which phase is meant.
+    static constexpr int STAGES = HD == 128 ? 2 : 4;
+    static constexpr int DYN_BYTES = (2 + 2 * STAGES) * TILE_BYTES + 1024;      // two tiles of queries: the streams', or this part's and the next one's
 };
+
+template <bool TMA>
+struct UmmaPagedRoles {
+    static constexpr int PROD = 8, MMA = TMA ? 9 : 12, QUERY = TMA ? 11 : 8, QUERY_WARPS = TMA ? 1 : 4;
+    static constexpr int THREADS = TMA ? 384 : 448;
+};
+// Keys of a tile that TMA brings, and whether it can: whole pages in 128 rows, or parts of 128 of a page.
+__host__ __device__ constexpr bool paged_tma_pages(int page_size) { return page_size % 8 == 0 && (page_size <= 128 || page_size % 128 == 0); }
+__host__ __device__ constexpr int paged_tma_keys(int page_size) { return page_size <= 128 ? 128 / page_size * page_size : 128; }
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+        : "memory");
+}
 
 // Operand descriptor of an MN-major tile in rows of 64 elements (128 bytes, 128-byte swizzle), 16 KB from one run of 64 to the next:
 // groups of eight rows along K are 1024 bytes apart.
@@ -82,51 +98,69 @@ struct PagedWalk {
     }
 };
 
-template <typename T, int HD, int MODE>
-__global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_kernel(const PagedArgs a) {
-    using SM = UmmaPagedSmem<HD, MODE>;
-    constexpr bool TWO = MODE == PAGED_TWO;
-    constexpr int KB = HD / 64, ST = SM::STAGES, TILE = kUmmaPagedTile;
-    constexpr int MT = TWO ? 256 : 128;
+template <typename T, int HD, int ROWS, bool TMA>
+__global__ void __launch_bounds__(UmmaPagedRoles<TMA>::THREADS, 1)
+paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV) {
+    using SM = UmmaPagedSmem<HD>;
+    using Role = UmmaPagedRoles<TMA>;
+    constexpr bool TWO = ROWS == 256;
+    constexpr int KB = HD / 64, ST = SM::STAGES, RING = TWO ? ST : ST / 2, TILE = kUmmaPagedTile, THREADS = Role::THREADS;
+    constexpr int MT = ROWS, REP = TWO ? 1 : 128 / ROWS, KC = 128 / REP;     // copies of a row, and keys of a tile that one takes
     constexpr uint32_t IDESC_S = umma_idesc16<T>(128, 128, false), IDESC_O = umma_idesc16<T>(128, HD, true);
     constexpr uint32_t O_COL = 256;              // scores of the streams at columns 0 and 128, accumulators at 256 and 384
     constexpr float kRaise = 8.f;
 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * SM::Q_BYTES, sV = sK + ST * SM::TILE_BYTES;
-    __shared__ uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], o_empty,
-        prod_bar, x_bar;
-    __shared__ uint64_t row_at[2][2 * TILE];     // addresses of a tile's key rows, then of its value rows; odd: no such row
+    const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * SM::TILE_BYTES, sV = sK + ST * SM::TILE_BYTES;
+    __shared__ uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], o_empty[2],
+        drain[2], tail_bar, prod_bar, x_bar, g_bar[2];
+    __shared__ uint64_t row_at[2][TMA ? 1 : 2 * TILE];     // by cp.async: addresses of a tile's key rows, then of its value rows; odd: no such row
     __shared__ uint64_t row_q[MT];
-    __shared__ float2 x_ml[2][2][128];           // !TWO: [parity of the part][stream][row] (maximum, sum)
+    __shared__ float2 x_ml[2][2][128];           // ROWS <= 128: [parity of the part][stream][row] (maximum, sum)
     __shared__ PagedRangeSmem range_smem;
     __shared__ uint32_t tmem_base_slot;
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, drain_flag;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        abort_flag = 0;
+        abort_flag = drain_flag = 0;
         for (int i = 0; i < ST; ++i) {
-            mbar_init(&k_full[i], 128);          // every producer thread's requests
-            mbar_init(&k_empty[i], 1);
-            mbar_init(&v_full[i], 128);
-            mbar_init(&v_empty[i], 1);
+            mbar_init(&k_full[i], TMA ? 1 : 128);          // by cp.async: every producer thread's requests
+            mbar_init(&k_empty[i], TWO ? 2 : 1);          // every stream that uses the tile
+            mbar_init(&v_full[i], TMA ? 1 : 128);
+            mbar_init(&v_empty[i], TWO ? 2 : 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&q_full[i], 128);
-            mbar_init(&q_empty[i], 1);
+            mbar_init(&q_full[i], Role::QUERY_WARPS * 32);
+            mbar_init(&q_empty[i], TWO ? 2 : 10);          // both streams' products; the softmax warps, which use the room at the end of a part
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
             mbar_init(&pv_done[i], 1);
+            mbar_init(&o_empty[i], TWO ? 4 : 8);         // the warps that read the accumulator
+            mbar_init(&drain[i], 1);
         }
-        mbar_init(&o_empty, 8);
-        mbar_init(&prod_bar, 4);
+        mbar_init(&prod_bar, Role::QUERY_WARPS);
         mbar_init(&x_bar, 8);
+        mbar_init(&tail_bar, 2);
+        mbar_init(&g_bar[0], 4);
+        mbar_init(&g_bar[1], 4);
         fence_barrier_init();
         fence_proxy_async_smem();
+        if (TMA) {
+            tma_prefetch_desc(&tmK);
+            tma_prefetch_desc(&tmV);
+        }
     }
-    if (warp == 12) {
+    const int KEYS = TMA ? paged_tma_keys(a.pages.page_size) : TILE;       // of a tile
+    if (TMA && KEYS < TILE) {                    // value rows that no box covers: their probabilities are zero, so they must be numbers
+        for (int i = tid; i < ST * KB * (TILE - KEYS) * 8; i += THREADS) {
+            const int c = i & 7, r = (i >> 3) % (TILE - KEYS), t = (i >> 3) / (TILE - KEYS);
+            *reinterpret_cast<uint4*>(smem + (sV - sQ) + t * 16384 + (KEYS + r) * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+    }
+    if (warp == Role::MMA) {
         tmem_alloc(&tmem_base_slot, 512);
         tmem_relinquish();
     }
@@ -140,7 +174,7 @@ __global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_ker
     grid_dependency_wait();
 
     const int R = a.T * a.group, RT = (R + MT - 1) / MT, per_b = a.nkv * RT;
-    const PagedRange rg = paged_range<T, HD, kUmmaPagedThreads>(a, TILE, per_b, range_smem);
+    const PagedRange rg = paged_range<T, HD, THREADS>(a, KEYS, per_b, range_smem);
     if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {
         const bool w = mbar_wait(bar, parity, abortp);
@@ -148,12 +182,73 @@ __global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_ker
     };
 
     if (rg.end > rg.begin) {
-        if (warp >= 8 && warp < 12) {
-            // ================================ producers ================================
-            const int pt = tid - 256, pw = pt >> 5;
+        if (TMA && warp == Role::PROD) {
+            // ================================ producer by TMA: lane = page of the tile ================================
+            const int ps = a.pages.page_size, boxes = ps <= 128 ? KEYS / ps : 1, box = min(ps, 128);
+            PagedWalk w(a, rg, KEYS);
+            PagedWalk ahead = w;                                   // the tile whose page entry is requested next
+            int ahead_j = 0;
+            bool ahead_more = true;
+            int page = 0;
+            auto request_entry = [&]() {
+                if (!ahead_more) return;
+                const int key = (ahead.kt + ahead_j) * KEYS + lane * box;
+                page = 0;
+                if (lane < boxes && key < ahead.n) page = a.table[ahead.b * a.table_stride + key / ps];
+                if (++ahead_j == ahead.cnt) {
+                    ahead_j = 0;
+                    ahead_more = ahead.next(a, per_b, KEYS);
+                }
+            };
+            request_entry();
+            uint32_t keys_sent[2] = {0, 0}, values_sent[2] = {0, 0};           // tiles per ring: a stream's, or both streams'
+            bool ok = true, more = true;
+            while (ok && more) {
+                const int head = w.item / RT;
+                for (int j = 0; j < w.cnt; ++j) {
+                    const int first = (w.kt + j) * KEYS, key = first + lane * box;
+                    const int here = min(boxes, (w.n - first + box - 1) / box);        // boxes that hold a key
+                    const bool real = lane < here;
+                    int pg = page;
+                    if (real && (unsigned)pg >= (unsigned)a.pages.n_pages) {
+                        if (a.status) atomicExch(a.status, kStatusBadIndex);
+                        pg = a.pages.n_pages;                      // past the map's end: zeros
+                    }
+                    const int off = ps <= 128 ? 0 : key % ps;
+                    request_entry();
+                    auto fetch = [&](uint32_t dst, const CUtensorMap* map, uint64_t* bar) {
+                        if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(here * box * HD * 2));
+                        __syncwarp();
+                        if (real) {
+#pragma unroll
+                            for (int kb = 0; kb < KB; ++kb) tma_load_4d(dst + kb * 16384 + lane * box * 128, map, bar, kb * 64, off, head, pg);
+                        }
+                        __syncwarp();
+                    };
+                    const int ring = TWO ? 0 : j & 1;
+                    const uint32_t at = keys_sent[ring], st = ring * RING + at % RING, ph = (at / RING & 1) ^ 1;
+                    if (!(ok = wait_all(&k_empty[st], ph))) break;
+                    fetch(sK + st * SM::TILE_BYTES, &tmK, &k_full[st]);
+                    ++keys_sent[ring];
+                    if (!(ok = wait_all(&v_empty[st], ph))) break;
+                    fetch(sV + st * SM::TILE_BYTES, &tmV, &v_full[st]);
+                    ++values_sent[ring];
+                }
+                if (ok) more = w.next(a, per_b, KEYS);
+            }
+            // somebody gave up: what is on its way must land before this CTA's shared memory is another's
+#pragma unroll
+            for (int i = 0; !ok && i < ST; ++i) {
+                const uint32_t nk = (keys_sent[i / RING] + RING - 1 - i % RING) / RING, nv = (values_sent[i / RING] + RING - 1 - i % RING) / RING;
+                if (nk > 0) mbar_wait(&k_full[i], (nk - 1) & 1, &drain_flag);
+                if (nv > 0) mbar_wait(&v_full[i], (nv - 1) & 1, &drain_flag);
+            }
+        } else if (warp >= Role::QUERY && warp < Role::QUERY + Role::QUERY_WARPS) {
+            // ================================ queries, and keys by cp.async ================================
+            const int pt = tid - Role::QUERY * 32, pw = pt >> 5;
             constexpr int CPR = HD / 8, RPP = 32 / CPR;            // chunks of a row; rows per request of a warp
             const int lr = lane / CPR, lc = lane % CPR;
-            uint32_t ldst[8 / RPP];                                // where this lane's chunk goes: repeats every 8 rows
+            uint32_t ldst[8 / RPP];                                // where this lane's chunk of a key goes: repeats every 8 rows
 #pragma unroll
             for (int i = 0; i < 8 / RPP; ++i)
                 ldst[i] = (uint32_t)((lc / 8) * 16384 + (pw * 32 + i * RPP + lr) * 128 + (((lc % 8) ^ ((i * RPP + lr) & 7)) << 4));
@@ -165,13 +260,12 @@ __global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_ker
                 }
             };
             auto copy_queries = [&](uint32_t dst, const uint64_t* rows) {
-                constexpr int ROWS = SM::Q_ROWS / 4;               // of this warp
-#pragma unroll
-                for (int i = 0; i < ROWS / RPP; ++i) {
-                    const int r = pw * ROWS + i * RPP + lr;
-                    const uint64_t at = rows[r];
-                    cp_async16(dst + (lc / 8) * (SM::Q_ROWS * 128) + r * 128 + (((lc % 8) ^ (r & 7)) << 4), reinterpret_cast<const uint8_t*>(at & ~1ull) + lc * 16,
-                               !(at & 1));
+                constexpr int SHARE = 128 / Role::QUERY_WARPS;     // rows of this warp
+#pragma unroll 8
+                for (int i = 0; i < SHARE / RPP; ++i) {
+                    const int r = pw * SHARE + i * RPP + lr;
+                    const uint64_t at = rows[TWO ? r : r % ROWS];
+                    cp_async16(dst + (lc / 8) * 16384 + r * 128 + (((lc % 8) ^ (r & 7)) << 4), reinterpret_cast<const uint8_t*>(at & ~1ull) + lc * 16, !(at & 1));
                 }
             };
             uint32_t prod_ph = 0;
@@ -226,33 +320,36 @@ __global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_ker
                 row_at[buf][pt] = ka;
                 row_at[buf][TILE + pt] = va;
             };
-            PagedWalk w(a, rg, TILE);
-            request_entry();
-            leave_address(0);
-            request_entry();
-            uint32_t g = 0, part = 0;                              // tiles and parts so far
+            PagedWalk w(a, rg, KEYS);
+            if (!TMA) {
+                request_entry();
+                leave_address(0);
+                request_entry();
+            }
+            uint32_t g = 0, part = 0, sent[2] = {0, 0};            // tiles and parts so far, tiles per ring
             bool ok = true, more = true;
             for (; ok && more; ++part) {
                 // queries of the part
                 const int head = w.item / RT, row0 = (w.item - head * RT) * MT;
                 const int qb = TWO ? 0 : (part & 1);
                 const uint32_t qph = TWO ? (part & 1) ^ 1 : ((part >> 1) & 1) ^ 1;
-#pragma unroll
-                for (int i = 0; i < MT / 128; ++i) {
-                    const int r = row0 + i * 128 + pt, t = r / a.group, gq = r - t * a.group;
+                for (int i = pt; i < MT; i += Role::QUERY_WARPS * 32) {
+                    const int r = row0 + i, t = r / a.group, gq = r - t * a.group;
                     uint64_t at = reinterpret_cast<uint64_t>(a.q) | 1u;
                     if (r < R) at = reinterpret_cast<uint64_t>((const T*)a.q + w.b * a.q_b + t * a.q_t + (int64_t)(head * a.group + gq) * a.q_h);
-                    row_q[i * 128 + pt] = at;
+                    row_q[i] = at;
                 }
                 ok = prod_sync();
                 if (ok) ok = wait_all(&q_empty[qb], qph);
                 if (!ok) break;
 #pragma unroll
-                for (int i = 0; i < (TWO ? 2 : 1); ++i) copy_queries(sQ + (TWO ? i : qb) * SM::Q_BYTES, row_q + i * 128);
+                for (int i = 0; i < (TWO ? 2 : 1); ++i) copy_queries(sQ + (TWO ? i : qb) * SM::TILE_BYTES, row_q + i * 128);
                 cp_async_arrive(&q_full[qb]);
-                for (int j = 0; j < w.cnt; ++j, ++g) {
-                    const int st = g % ST, buf = g & 1;
-                    const uint32_t ph = ((g / ST) & 1) ^ 1;
+                if (TMA && !(ok = prod_sync())) break;             // the addresses are used up
+                for (int j = 0; !TMA && j < w.cnt; ++j, ++g) {
+                    const int buf = g & 1, ring = TWO ? 0 : j & 1;
+                    const uint32_t st = ring * RING + sent[ring] % RING, ph = (sent[ring] / RING & 1) ^ 1;
+                    ++sent[ring];
                     ok = prod_sync();                              // the tile's addresses are there, the ones before are used up
                     if (ok) ok = wait_all(&k_empty[st], ph);
                     if (!ok) break;
@@ -264,116 +361,150 @@ __global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_ker
                     copy_rows(sV + st * SM::TILE_BYTES, row_at[buf] + TILE);
                     cp_async_arrive(&v_full[st]);
                 }
-                if (ok) more = w.next(a, per_b, TILE);
+                if (ok) more = w.next(a, per_b, KEYS);
             }
-        } else if (warp == 12) {
-            // ================================ MMA issuer ================================
+        } else if (warp == Role::MMA || warp == Role::MMA + 1) {
+            // ================================ products of stream s ================================
+            const int s = warp - Role::MMA;
             const bool elected = elect_one();
-            const uint64_t qd0 = umma_desc_k128(sQ), kd0 = umma_desc_k128(sK), vd0 = umma_desc_mn128(sV);
-            PagedWalk w(a, rg, TILE);
-            uint32_t g0 = 0, part = 0, done[2] = {0, 0};           // tiles before this part; second products per stream so far
+            const uint64_t qd0 = umma_desc_k128(sQ) + (uint64_t)(TWO ? s * (SM::TILE_BYTES >> 4) : 0), kd0 = umma_desc_k128(sK), vd0 = umma_desc_mn128(sV);
+            const uint32_t d_s = tmem_base + s * 128, d_o = tmem_base + O_COL + s * 128;
+            PagedWalk w(a, rg, KEYS);
+            uint32_t part = 0, used = 0, made = 0, done = 0, tails = 0;        // parts, those with a tile of this stream, first and second products, tails so far
             bool ok = true, more = true;
             for (; ok && more; ++part) {
-                const int units = TWO ? 2 * w.cnt : w.cnt;
+                const int units = TWO ? w.cnt : (w.cnt + 1 - s) / 2;                  // tiles of this stream
                 const int qb = TWO ? 0 : (part & 1);
+                const int tail = w.n - (w.nt - 1) * KEYS;          // keys of the last tile of the sequence
+                const bool has_tail = TMA && w.kt + w.cnt == w.nt && tail < KEYS;
                 ok = wait_all(&q_full[qb], TWO ? (part & 1) : ((part >> 1) & 1));
-                uint32_t made[2] = {0, 0};                         // second products of this part
+                if (ok) fence_proxy_async_smem();                  // the queries are written as threads write; the tensor pipe reads as copies do
                 auto issue_S = [&](int u) -> bool {
-                    const int s = u & 1, tile = TWO ? u >> 1 : u;
-                    const uint32_t g = g0 + tile, st = g % ST;
-                    if (!wait_all(&k_full[st], (g / ST) & 1)) return false;
+                    const uint32_t st = (TWO ? 0 : s * RING) + made % RING;
+                    if (!wait_all(&k_full[st], made / RING & 1)) return false;
                     // the score buffer holds the probabilities of the stream's previous tile until its second product is done
-                    const uint32_t before = done[s];
-                    if (before > 0 && !wait_all(&pv_done[s], (before - 1) & 1)) return false;
-                    fence_proxy_async_smem();                      // the requests wrote as threads do; the tensor pipe reads as copies do
+                    if (done > 0 && !wait_all(&pv_done[s], (done - 1) & 1)) return false;
+                    if (!TMA) fence_proxy_async_smem();
                     tc_fence_after();
                     if (elected) {
-                        const uint64_t qd = qd0 + (uint64_t)((TWO ? s : qb) * (SM::Q_BYTES >> 4)), kd = kd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
+                        const uint64_t qd = qd0 + (uint64_t)(TWO ? 0 : qb * (SM::TILE_BYTES >> 4)), kd = kd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
 #pragma unroll
                         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                umma_bf16(tmem_base + s * 128, qd + kb * (SM::Q_ROWS * 8) + 2 * k, kd + kb * 1024 + 2 * k, IDESC_S, (kb | k) != 0);
+                            for (int k = 0; k < 4; ++k) umma_bf16(d_s, qd + kb * 1024 + 2 * k, kd + kb * 1024 + 2 * k, IDESC_S, (kb | k) != 0);
                         umma_commit(&s_full[s]);
-                        if (!TWO || s == 1) umma_commit(&k_empty[st]);
+                        umma_commit(&k_empty[st]);
                         if (u == units - 1) umma_commit(&q_empty[qb]);
                     }
                     __syncwarp();
+                    ++made;
                     return true;
                 };
                 auto issue_PV = [&](int u) -> bool {
-                    const int s = u & 1, tile = TWO ? u >> 1 : u;
-                    const uint32_t g = g0 + tile, st = g % ST;
-                    if (!wait_all(&v_full[st], (g / ST) & 1)) return false;
-                    if (!wait_all(&p_full[s], done[s] & 1)) return false;
-                    // the part's first products overwrite the accumulators: the previous part's rows must have left
-                    if (u == 0 && part > 0 && !wait_all(&o_empty, (part - 1) & 1)) return false;
-                    fence_proxy_async_smem();
+                    const int tile = TWO ? u : 2 * u + s;
+                    const uint32_t st = (TWO ? 0 : s * RING) + done % RING;
+                    if (!wait_all(&v_full[st], done / RING & 1)) return false;
+                    if (has_tail && tile == w.cnt - 1) {
+                        // value rows behind the sequence's end, whatever the page holds there, and those of boxes that were not fetched
+                        if (!TWO || s == 0) {
+                            for (int i = lane; i < KB * (KEYS - tail) * 8; i += 32) {
+                                const int r = tail + (i >> 3) % (KEYS - tail), kb = (i >> 3) / (KEYS - tail);
+                                *reinterpret_cast<uint4*>(smem + (sV - sQ) + st * SM::TILE_BYTES + kb * 16384 + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                        }
+                        if (TWO) {                                 // the streams' warps meet: both see the zeros, and neither is a tail ahead
+                            if (lane == 0) mbar_arrive(&tail_bar);
+                            if (!wait_all(&tail_bar, tails & 1)) return false;
+                        }
+                    }
+                    if (!wait_all(&p_full[s], done & 1)) return false;
+                    if (!TMA) fence_proxy_async_smem();
                     tc_fence_after();
                     if (elected) {
                         const uint64_t vd = vd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            umma_bf16_ts(tmem_base + O_COL + s * 128, tmem_base + s * 128 + (k < 4 ? 8 * k : 64 + 8 * (k - 4)), vd + k * 128, IDESC_O,
-                                         made[s] > 0 || k > 0);
+                        for (int k = 0; k < 8; ++k) umma_bf16_ts(d_o, d_s + (k < 4 ? 8 * k : 64 + 8 * (k - 4)), vd + k * 128, IDESC_O, u > 0 || k > 0);
                         umma_commit(&pv_done[s]);
-                        if (!TWO || s == 1) umma_commit(&v_empty[st]);
+                        umma_commit(&v_empty[st]);
                     }
                     __syncwarp();
-                    ++made[s];
-                    ++done[s];
+                    ++done;
                     return true;
                 };
-                if (ok) ok = issue_S(0);
-                if (ok && units > 1) ok = issue_S(1);
+                if (ok && units > 0) ok = issue_S(0);
+                if (ok && units == 0 && lane == 0) mbar_arrive(&q_empty[qb]);
+                // the part's first products overwrite the accumulator: the previous part's rows must have left
+                if (ok && units > 0 && used++ > 0) ok = wait_all(&o_empty[s], (used - 2) & 1);
                 for (int u = 0; ok && u < units; ++u) {
                     ok = issue_PV(u);
-                    if (ok && u + 2 < units) ok = issue_S(u + 2);
+                    if (ok && u + 1 < units) ok = issue_S(u + 1);
                 }
-                g0 += w.cnt;
-                if (ok) more = w.next(a, per_b, TILE);
+                tails += has_tail;
+                if (ok) more = w.next(a, per_b, KEYS);
             }
-            // the last arrival the tensor pipe owes this CTA's barriers
-            if (ok) wait_all(&v_empty[(g0 - 1) % ST], ((g0 - 1) / ST) & 1);
+            // the last arrivals the tensor pipe owes this CTA's barriers; where somebody gave up, the end of the products under way
+            if (ok) {
+                if (done > 0) wait_all(&v_empty[(TWO ? 0 : s * RING) + (done - 1) % RING], (done - 1) / RING & 1);
+            } else {
+                if (elected) umma_commit(&drain[s]);
+                __syncwarp();
+                mbar_wait(&drain[s], 0, &drain_flag);
+            }
         } else {
             // ================================ softmax: thread = row of its stream ================================
             const int s = warp >> 2, quad = warp & 3, r128 = quad * 32 + lane;
+            const int rep = TWO ? 0 : r128 / ROWS, wr = TWO ? s * 128 + quad * 32 : quad * 32 % ROWS;      // copy of the row; first row of the warp
             const uint32_t lanes = tmem_base + (uint32_t(quad * 32) << 16), sc = lanes + s * 128;
-            const float c = a.scale_log2;
-            PagedWalk w(a, rg, TILE);
-            uint32_t done[2] = {0, 0}, part = 0;                   // tiles of each stream so far
+            const float c = a.scale_log2, none = c < 0.f ? INFINITY : -INFINITY;
+            PagedWalk w(a, rg, KEYS);
+            uint32_t done[2] = {0, 0}, part = 0, g_ph = 0;         // tiles of each stream so far
             bool ok = true, more = true;
             for (; ok && more; ++part) {
                 const int head = w.item / RT, row0 = (w.item - head * RT) * MT;
-                const int wrow = row0 + (TWO ? s * 128 : 0) + quad * 32;           // first row of this warp
-                const bool idle = wrow >= R;                                       // none of its rows exists: it only keeps the barriers going
+                const bool idle = row0 + wr >= R;                  // none of the warp's rows exists: it only keeps the barriers going
                 const int mine = TWO ? w.cnt : (w.cnt + 1 - s) / 2, other = TWO ? w.cnt : (w.cnt + s) / 2;
                 float mc = -INFINITY, l = 0.f;
                 for (int i = 0; i < mine; ++i) {
                     if (!(ok = wait_all(&s_full[s], (done[s] + i) & 1))) break;
                     if (!idle) {
                         tc_fence_after();
-                        const int tile = w.kt + (TWO ? i : 2 * i + s), limit = w.n - tile * TILE;      // keys of the tile that exist
-                        const float none = c < 0.f ? INFINITY : -INFINITY;
+                        // keys of the tile that exist, from the first one of this copy on
+                        const int limit = min(w.n - (w.kt + (TWO ? i : 2 * i + s)) * KEYS, KEYS) - rep * KC;
                         float v[64], bm = none;
-                        // the maximum: keys 0..63, then 64..127, which stay in registers
+                        auto maximum = [&](float* x, int first, int count) {
+                            if (limit < first + count) {
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            tmem_ld32(sc + half * 64, v);
-                            tmem_ld32(sc + half * 64 + 32, v + 32);
-                            tmem_ld_wait_regs(v);
-                            tmem_ld_wait_regs(v + 32);
-                            if (limit < TILE) {
-#pragma unroll
-                                for (int t = 0; t < 64; ++t)
-                                    if (half * 64 + t >= limit) v[t] = none;
+                                for (int t = 0; t < count; ++t)
+                                    if (first + t >= limit) x[t] = none;
                             }
                             if (c < 0.f) {
 #pragma unroll
-                                for (int t = 0; t < 64; ++t) bm = fminf(bm, v[t]);
+                                for (int t = 0; t < count; ++t) bm = fminf(bm, x[t]);
                             } else {
+                                float b1 = none;
 #pragma unroll
-                                for (int t = 0; t < 64; t += 2) bm = fmaxf(bm, fmaxf(v[t], v[t + 1]));
+                                for (int t = 0; t < count; t += 4) {
+                                    bm = fmaxf(bm, fmaxf(x[t], x[t + 1]));
+                                    b1 = fmaxf(b1, fmaxf(x[t + 2], x[t + 3]));
+                                }
+                                bm = fmaxf(bm, b1);
+                            }
+                        };
+                        if (KC == 32) {
+                            tmem_ld32(sc + rep * 32, v);
+                            tmem_ld_wait_regs(v);
+                            maximum(v, 0, 32);
+                        } else {
+                            // with a whole row per thread: keys 0..63, then 64..127, which stay in registers
+#pragma unroll
+                            for (int half = 0; half < KC / 64; ++half) {
+                                tmem_ld32(sc + rep * KC + half * 64, v);
+                                tmem_ld32(sc + rep * KC + half * 64 + 32, v + 32);
+                                tmem_ld_wait_regs(v);
+                                tmem_ld_wait_regs(v + 32);
+                                maximum(v, half * 64, 64);
                             }
                         }
                         const float bmc = bm * c;
@@ -384,8 +515,7 @@ __global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_ker
                         l *= f;
                         const float base = mc == -INFINITY ? 0.f : mc;
                         float l0 = 0.f, l1 = 0.f;
-                        // 32 scores -> 16 columns of probabilities.  Keys 64..127 go to columns 64..95, whose scores have just been read, keys
-                        // 0..63 to columns 0..31, behind the reads of theirs.
+                        // 32 scores -> 16 columns of probabilities: keys 0..63 of the tile in columns 0..31, 64..127 in columns 64..95
                         auto probabilities = [&](const float* x, uint32_t col) {
                             uint32_t packed[16];
 #pragma unroll
@@ -398,24 +528,33 @@ __global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_ker
                             }
                             tmem_st16(sc + col, packed);
                         };
-                        probabilities(v, 64);
-                        tmem_ld32(sc, v);
-                        probabilities(v + 32, 80);
-                        tmem_ld_wait_regs(v);
-                        tmem_ld32(sc + 32, v + 32);
-                        if (limit < 64) {
+                        if (KC < 128) {
+                            const uint32_t zeros[16] = {};
 #pragma unroll
-                            for (int t = 0; t < 32; ++t)
-                                if (t >= limit) v[t] = none;
+                            for (int q = 0; q < 4; ++q)            // the other copies' keys
+                                if (q / (KC / 32) != rep) tmem_st16(sc + (q >> 1) * 64 + (q & 1) * 16, zeros);
                         }
-                        probabilities(v, 0);
-                        tmem_ld_wait_regs(v + 32);
-                        if (limit < 64) {
+                        if (KC == 32) {
+                            probabilities(v, (rep >> 1) * 64 + (rep & 1) * 16);
+                        } else if (KC == 64) {
+                            probabilities(v, rep * 64);
+                            probabilities(v + 32, rep * 64 + 16);
+                        } else {
+                            // (columns 64..95 held scores that have just been read, columns 0..31 are written behind the reads of theirs)
+                            probabilities(v, 64);
+                            probabilities(v + 32, 80);
+                            tmem_ld32(sc, v);
+                            tmem_ld32(sc + 32, v + 32);
+                            tmem_ld_wait_regs(v);
+                            tmem_ld_wait_regs(v + 32);
+                            if (limit < 64) {
 #pragma unroll
-                            for (int t = 0; t < 32; ++t)
-                                if (32 + t >= limit) v[32 + t] = none;
+                                for (int t = 0; t < 64; ++t)
+                                    if (t >= limit) v[t] = none;
+                            }
+                            probabilities(v, 0);
+                            probabilities(v + 32, 16);
                         }
-                        probabilities(v + 32, 16);
                         l += l0 + l1;
                         if (__any_sync(0xffffffffu, shrink)) {
                             // (the previous second product of this stream was done before these scores were made)
@@ -441,83 +580,171 @@ __global__ void __launch_bounds__(kUmmaPagedThreads, 1) paged_attention_umma_ker
                 // ---- the part goes out ----
                 const bool begins = w.kt == 0, whole = begins && w.cnt == w.nt;
                 const int64_t slot = (int64_t)blockIdx.x * 2 + (begins ? 1 : 0);
-                const int r = row0 + (TWO ? s * 128 : 0) + r128, rt = r - row0, t = r / a.group, gq = r - t * a.group;
-                float wa = 0.f, wb = 0.f, m = mc, sum = l;         // weights of stream 0's and stream 1's accumulators
+                // rt: row within the item; 32 columns of it: x
+                auto put = [&](int rt, int col, const float* x, int count) {
+                    const int r = row0 + rt, t = r / a.group, gq = r - t * a.group;
+                    if (whole) {
+                        T* dst = (T*)a.out + w.b * a.o_b + t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + col;
+                        if (count == 4) {
+                            typename Pack2<T>::type lo = Pack2<T>::down(x[0], x[1]), hi = Pack2<T>::down(x[2], x[3]);
+                            *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < count / 8; ++e) reinterpret_cast<uint4*>(dst)[e] = pack8<T>(x + 8 * e);
+                        }
+                    } else {
+                        float4* dst = reinterpret_cast<float4*>(a.partial + (slot * MT + rt) * HD + col);
+#pragma unroll
+                        for (int e = 0; e < count / 4; ++e) dst[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+                    }
+                };
+                auto put_ml = [&](int rt, float m, float sum) {
+                    const int r = row0 + rt, t = r / a.group, gq = r - t * a.group;
+                    if (!whole) a.partial_ml[slot * MT + rt] = make_float2(m, sum);
+                    else if (a.lse) a.lse[((int64_t)w.b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(sum)) * 0.69314718055994531f;
+                };
                 if (TWO) {
-                    wa = 1.f;
-                    ok = wait_all(&pv_done[s], (done[s] - 1) & 1);
+                    // thread = row
+                    if (!(ok = wait_all(&pv_done[s], (done[s] - 1) & 1))) break;
+                    const int rt = s * 128 + r128;
+                    const bool real = row0 + rt < R;
+                    if (!idle) {
+                        tc_fence_after();
+                        const float weight = whole ? 1.f / l : 1.f;
+#pragma unroll
+                        for (int ch = 0; ch < HD / 32; ++ch) {
+                            float o[32];
+                            tmem_ld32(lanes + O_COL + s * 128 + ch * 32, o);
+                            tmem_ld_wait_regs(o);
+#pragma unroll
+                            for (int x = 0; x < 32; ++x) o[x] *= weight;
+                            if (real) put(rt, ch * 32, o, 32);
+                        }
+                        if (real) put_ml(rt, mc, l);
+                        tc_fence_before();
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&o_empty[s]);
                 } else {
+                    // The streams and the copies of a row meet: each thread weighs what its lane holds in both accumulators, half of the columns
+                    // a warpgroup, and the copies are added up through the room of this part's queries, which are used up.
                     x_ml[part & 1][s][r128] = make_float2(mc, l);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&x_bar);
                     ok = wait_all(&x_bar, part & 1);
                     if (ok) ok = wait_all(&pv_done[0], (done[0] - 1) & 1);
                     if (ok && w.cnt > 1) ok = wait_all(&pv_done[1], (done[1] - 1) & 1);
-                    if (ok) {
-                        const float2 x0 = x_ml[part & 1][0][r128], x1 = x_ml[part & 1][1][r128];
-                        m = fmaxf(x0.x, x1.x);
-                        const float mb = m == -INFINITY ? 0.f : m;
-                        wa = ex2_approx(x0.x - mb);
-                        wb = w.cnt > 1 ? ex2_approx(x1.x - mb) : 0.f;
-                        sum = x0.y * wa + (w.cnt > 1 ? x1.y * wb : 0.f);
-                        if (m == -INFINITY) wa = wb = 1.f;         // nothing but scores of minus infinity, or NaN
-                    }
-                }
-                if (!ok) break;
-                if (!idle) {
-                    tc_fence_after();
-                    const float inv = whole ? 1.f / sum : 1.f;
-                    wa *= inv;
-                    wb *= inv;
-                    constexpr int COLS = TWO ? HD : HD / 2;        // columns of this thread: all of its own row, or half of the shared one
-                    const int col0 = TWO ? 0 : s * (HD / 2);
+                    if (!ok) break;
+                    const bool both = w.cnt > 1;
+                    auto meet = [&](int rt, float& m, float& sum) {            // maximum and sum over everything that has keys of row rt
+                        m = -INFINITY;
+                        sum = 0.f;
 #pragma unroll
-                    for (int ch = 0; ch < COLS / 32; ++ch) {
-                        float o[32];
-                        const int col = col0 + ch * 32;
-                        tmem_ld32(lanes + O_COL + (TWO ? s * 128 : 0) + col, o);
-                        tmem_ld_wait_regs(o);
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) o[x] *= wa;
-                        if (!TWO && w.cnt > 1) {
-                            float o2[32];
-                            tmem_ld32(lanes + O_COL + 128 + col, o2);
-                            tmem_ld_wait_regs(o2);
-#pragma unroll
-                            for (int x = 0; x < 32; ++x) o[x] += o2[x] * wb;
+                        for (int q = 0; q < REP; ++q) {
+                            m = fmaxf(m, x_ml[part & 1][0][q * ROWS + rt].x);
+                            if (both) m = fmaxf(m, x_ml[part & 1][1][q * ROWS + rt].x);
                         }
-                        if (r < R) {
-                            if (whole) {
-                                uint4* dst = reinterpret_cast<uint4*>((T*)a.out + w.b * a.o_b + t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + col);
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) dst[x] = pack8<T>(o + 8 * x);
+                        for (int q = 0; q < REP; ++q) {
+                            const float2 x0 = x_ml[part & 1][0][q * ROWS + rt], x1 = x_ml[part & 1][1][q * ROWS + rt];
+                            sum += x0.y * (m == -INFINITY ? 1.f : ex2_approx(x0.x - m));
+                            if (both) sum += x1.y * (m == -INFINITY ? 1.f : ex2_approx(x1.x - m));
+                        }
+                    };
+                    float* room = reinterpret_cast<float*>(smem + (part & 1) * SM::TILE_BYTES + s * (SM::TILE_BYTES / 2));
+                    constexpr int ROUND = HD / 4, ROUNDS = 2, CH4 = ROUND / 4;       // columns of a round, 16-byte chunks of them
+                    float wa = 0.f, wb = 0.f;
+                    if (!idle) {
+                        float m, sum;
+                        const int rt = r128 % ROWS;
+                        meet(rt, m, sum);
+                        wa = m == -INFINITY ? 1.f : ex2_approx(x_ml[part & 1][0][r128].x - m);
+                        wb = m == -INFINITY ? 1.f : ex2_approx(x_ml[part & 1][1][r128].x - m);
+                        tc_fence_after();
+                    }
+#pragma unroll
+                    for (int round = 0; round < ROUNDS; ++round) {
+                        const int col = s * (HD / 2) + round * ROUND;
+                        if (!idle) {
+                            float o[32], o2[32];
+                            if (ROUND == 32) {
+                                tmem_ld32(lanes + O_COL + col, o);
+                                if (both) tmem_ld32(lanes + O_COL + 128 + col, o2);
+                                tmem_ld_wait_regs(o);
+                                if (both) tmem_ld_wait_regs(o2);
                             } else {
-                                float4* dst = reinterpret_cast<float4*>(a.partial + (slot * MT + rt) * HD + col);
 #pragma unroll
-                                for (int x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+                                for (int e = 0; e < ROUND / 8; ++e) {
+                                    tmem_ld8(lanes + O_COL + col + 8 * e, o + 8 * e);
+                                    if (both) tmem_ld8(lanes + O_COL + 128 + col + 8 * e, o2 + 8 * e);
+                                }
+#pragma unroll
+                                for (int e = 0; e < ROUND / 8; ++e) {
+                                    tmem_ld8_wait(o + 8 * e);
+                                    if (both) tmem_ld8_wait(o2 + 8 * e);
+                                }
+                            }
+#pragma unroll
+                            for (int x = 0; x < ROUND; ++x) o[x] = both ? o[x] * wa + o2[x] * wb : o[x] * wa;
+#pragma unroll
+                            for (int e = 0; e < CH4; ++e)
+                                reinterpret_cast<float4*>(room + r128 * ROUND)[e ^ (lane & (CH4 - 1))] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        }
+                        if (round == ROUNDS - 1) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) {
+                                mbar_arrive(&o_empty[0]);
+                                if (both) mbar_arrive(&o_empty[1]);
                             }
                         }
+                        // the warpgroup's rows are in the room
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&g_bar[s]);
+                        if (!(ok = wait_all(&g_bar[s], g_ph))) break;
+                        g_ph ^= 1;
+                        for (int i = tid & 127; i < min(ROWS, R - row0) * CH4; i += 128) {
+                            const int rt = i / CH4, e = i % CH4;
+                            float x[4] = {};
+#pragma unroll
+                            for (int q = 0; q < REP; ++q) {
+                                const int rr = q * ROWS + rt;
+                                const float4 y = reinterpret_cast<const float4*>(room + rr * ROUND)[e ^ (rr & (CH4 - 1))];
+                                x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w;
+                            }
+                            float m, sum;
+                            meet(rt, m, sum);
+                            if (whole) {
+                                const float inv = 1.f / sum;
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) x[k] *= inv;
+                            }
+                            put(rt, col + 4 * e, x, 4);
+                            if (s == 0 && round == 0 && e == 0) put_ml(rt, m, sum);
+                        }
+                        __syncwarp();
+                        if (round + 1 < ROUNDS) {
+                            if (lane == 0) mbar_arrive(&g_bar[s]);
+                            if (!(ok = wait_all(&g_bar[s], g_ph))) break;
+                            g_ph ^= 1;
+                        }
                     }
-                    if (r < R && (TWO || s == 0)) {
-                        if (!whole) a.partial_ml[slot * MT + rt] = make_float2(m, sum);
-                        else if (a.lse) a.lse[((int64_t)w.b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(sum)) * 0.69314718055994531f;
-                    }
-                    tc_fence_before();
+                    if (!ok) break;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&q_empty[part & 1]);
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&o_empty);
                 if (begins && !whole && tid == 0) {
                     const int64_t last = rg.end + (w.nt - w.cnt) - 1;
                     a.desc[blockIdx.x] = make_int4(w.b, w.item, paged_owner(rg.total, rg.ctas, last) - (int)blockIdx.x + 1, 0);
                 }
-                more = w.next(a, per_b, TILE);
+                more = w.next(a, per_b, KEYS);
             }
         }
     }
     cp_async_wait<0>();
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == Role::MMA) {
         tc_fence_after();
         tmem_dealloc(tmem_base, 512);
     }

@@ -265,6 +265,14 @@ ATTENTION_CASES = [
     (5, 5, 1, 128, 7, FP16, [1, 2, 3, 4, 5, 6, 7, 8]),
     (1, 8, 1, 64, 16, BF16, [(i * 37) % 300 - 5 for i in range(301)]),      # more sequences than a CTA has threads
     (20, 8, 8, 128, 32, FP16, [(i * 53) % 400 for i in range(40)]),
+    (40, 4, 2, 64, 10, BF16, [300, 128, 129, 0]),           # pages of no multiple of eight keys: 80 and 192 rows
+    (64, 6, 2, 128, 100, FP16, [450, 3]),
+    (20, 4, 4, 128, 256, BF16, [700, 256, 255, 1]),         # pages larger than a tile
+    (150, 2, 1, 64, 256, FP16, [1025, 130]),
+    (50, 2, 2, 128, 8, BF16, [333, 128, 120, 121]),         # sixteen pages a tile
+    (33, 2, 2, 64, 56, FP16, [112, 113, 500]),              # tiles of two pages with room behind them
+    (18, 1, 1, 128, 120, BF16, [121, 240]),
+    (20, 4, 4, 64, 200, BF16, [401, 77]),
 ]
 
 
