@@ -114,12 +114,15 @@ PagedSpace paged_space(int row_tile, int head_dim) {
     return s;
 }
 
-// The second kernel: four warps to a row where an item may be in many parts (few items on many CTAs), a warp to a row otherwise.
+// The second kernel: four warps to a row where an item may be in many parts (few items on many CTAs), else a warp to a row, or to
+// four where there are many rows (their requests are in flight together: 224 rows of eight sequences, 20 MB of parts).
 template <typename T, int HD>
 int launch_join(const PagedArgs& a, int grid, int row_tile, cudaStream_t st) {
     const int all = a.T * a.group, rows = std::min(row_tile, all), row_tiles = (all + row_tile - 1) / row_tile;
-    if (grid > 8ll * a.B * a.nkv * row_tiles) launch_k((paged_join_kernel<T, HD, 1>), dim3((unsigned)grid, (unsigned)rows), dim3(kPagedThreads), 0, st, a, row_tile);
-    else launch_k((paged_join_kernel<T, HD, 4>), dim3((unsigned)grid, (unsigned)((rows + 3) / 4)), dim3(kPagedThreads), 0, st, a, row_tile);
+    auto go = [&](auto* kernel, int per_cta) { launch_k(kernel, dim3((unsigned)grid, (unsigned)((rows + per_cta - 1) / per_cta)), dim3(kPagedThreads), 0, st, a, row_tile); };
+    if (grid > 8ll * a.B * a.nkv * row_tiles) go(paged_join_kernel<T, HD, 4, 1>, 1);
+    else if (rows <= 32) go(paged_join_kernel<T, HD, 1, 1>, 4);
+    else go(paged_join_kernel<T, HD, 1, 4>, 16);
     return launch_check();
 }
 
@@ -329,6 +332,8 @@ int jot_paged_attention(const void* d_q, int64_t q_seq_stride, int64_t q_row_str
     const int64_t row_tiles = (rows + row_tile - 1) / row_tile, items = row_tiles * pages->n_kv_heads;
     const int64_t most_keys = (int64_t)max_pages * pages->page_size;
     if (items > INT32_MAX || most_keys > INT32_MAX - kUmmaPagedTile) return JOT_ERR_SHAPE;
+    // the line of tiles, were every sequence as long as its table allows, counted in 31 bits
+    if ((most_keys / 64 + 1) * items > INT32_MAX / B) return JOT_ERR_SHAPE;
     DeviceInfo* di = nullptr;
     JOT_TRY(device_info(&di));
     PagedArgs a{};

@@ -90,21 +90,22 @@ __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) {
     return n > most ? (int)most : n;
 }
 
-// Where a CTA's share of the line of tiles begins.
+// The share of a CTA on the line of tiles (fewer than 2^31, which the host makes sure of), and where it begins.
 struct PagedRange {
-    int64_t begin, end, total;      // tiles of the line
+    int begin, end, total;          // tiles of the line
     int ctas;                       // CTAs that have a share
-    int b;                          // sequence of the first tile, and the tile within the sequence
-    int64_t in_seq;
+    int b, n, item, kt;             // sequence of the first tile, its keys; item within the sequence; tile within the item
 };
 
-__host__ __device__ __forceinline__ int64_t paged_share(int64_t total, int ctas, int i) { return total * i / ctas; }
-// the CTA that has tile t
-__host__ __device__ __forceinline__ int paged_owner(int64_t total, int ctas, int64_t t) { return (int)(((t + 1) * ctas - 1) / total); }
+// total tiles over `ctas` CTAs, the first total % ctas of them one more: where CTA i's begin, and whose tile t is
+__host__ __device__ __forceinline__ int paged_share(int total, int ctas, int i) { return total / ctas * i + (i < total % ctas ? i : total % ctas); }
+__host__ __device__ __forceinline__ int paged_owner(int total, int ctas, int t) {
+    const int q = total / ctas, longer = total % ctas, edge = longer * (q + 1);
+    return t < edge ? t / (q + 1) : longer + (t - edge) / q;
+}
 
 struct PagedRangeSmem {
-    int64_t warp_tot[16], in_seq;
-    int b;
+    int warp_tot[16], b, in_seq;
 };
 
 // The share of this CTA on the line of tiles of `tile` keys, per_b items a sequence; sequences without a key are answered here:
@@ -113,62 +114,79 @@ template <typename T, int HD, int THREADS>
 __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, int per_b, PagedRangeSmem& sm) {
     constexpr int WARPS = THREADS / 32, CPR = HD / 8;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    auto tiles_of = [&](int b) -> int64_t {
-        const int n = b < a.B ? paged_len(a, b) : 0;
-        return n > 0 ? (int64_t)((n + tile - 1) / tile) * per_b : 0;
+    bool empty = false;             // whether a sequence of this thread has no key
+    auto tiles_of = [&](int b) -> int {
+        if (b >= a.B) return 0;
+        const int n = paged_len(a, b);
+        empty |= n == 0;
+        if (blockIdx.x == 0 && a.status && a.lens[b] > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
+        return n > 0 ? (n + tile - 1) / tile * per_b : 0;
     };
-    auto totals = [&]() {
-        int64_t t = 0;
+    auto scan = [&](int v) {        // inclusive, over the warp
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) t += sm.warp_tot[w];
-        return t;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += up;
+        }
+        return v;
     };
     PagedRange rg;
-    const int64_t first = tiles_of(tid);
-    int64_t sum = first;
-    bool empty = false;
-    for (int b = tid; b < a.B; b += THREADS) {
-        if (b != tid) sum += tiles_of(b);
-        const int n = a.lens[b];
-        empty |= paged_len(a, b) == 0;
-        if (blockIdx.x == 0 && a.status && n > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) sm.warp_tot[warp] = sum;
-    empty = __syncthreads_or(empty);
-    rg.total = totals();
-    rg.ctas = (int)min((int64_t)gridDim.x, rg.total);
-    rg.begin = rg.end = rg.in_seq = 0;
-    rg.b = 0;
-    if ((int)blockIdx.x < rg.ctas) {
-        rg.begin = paged_share(rg.total, rg.ctas, blockIdx.x);
-        rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
-        int64_t before = 0;
-        for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-            const int64_t mine = b0 == 0 ? first : tiles_of(b0 + tid);
-            int64_t inc = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
-                if (lane >= o) inc += up;
-            }
-            __syncthreads();                                        // warp_tot is read by everyone before it is written again
-            if (lane == 31) sm.warp_tot[warp] = inc;
-            __syncthreads();
-            int64_t start = before + inc - mine;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) start += w < warp ? sm.warp_tot[w] : 0;
-            if (start <= rg.begin && rg.begin < start + mine) {
-                sm.b = b0 + tid;
-                sm.in_seq = rg.begin - start;
-            }
-            before += totals();
-            if (before > rg.begin) break;
+    int in_seq = 0;
+    const int first = tiles_of(a.B <= 32 ? lane : tid);
+    if (a.B <= 32) {                // every warp for itself
+        const int inc = scan(first);
+        rg.total = __shfl_sync(0xffffffffu, inc, 31);
+        rg.ctas = min((int)gridDim.x, rg.total);
+        empty = __any_sync(0xffffffffu, empty);
+        rg.begin = rg.end = rg.b = 0;
+        if ((int)blockIdx.x < rg.ctas) {
+            rg.begin = paged_share(rg.total, rg.ctas, blockIdx.x);
+            rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
+            rg.b = __popc(__ballot_sync(0xffffffffu, inc <= rg.begin));        // sequences that end before it
+            in_seq = rg.begin - __shfl_sync(0xffffffffu, inc - first, rg.b);
         }
-        __syncthreads();
-        rg.b = sm.b;
-        rg.in_seq = sm.in_seq;
+    } else {
+        int sum = first;
+        for (int b = tid + THREADS; b < a.B; b += THREADS) sum += tiles_of(b);
+        sum = scan(sum);
+        if (lane == 31) sm.warp_tot[warp] = sum;
+        empty = __syncthreads_or(empty);
+        auto totals = [&](int warps) {
+            int t = 0;
+            for (int w = 0; w < warps; ++w) t += sm.warp_tot[w];
+            return t;
+        };
+        rg.total = totals(WARPS);
+        rg.ctas = min((int)gridDim.x, rg.total);
+        rg.begin = rg.end = rg.b = 0;
+        if ((int)blockIdx.x < rg.ctas) {
+            rg.begin = paged_share(rg.total, rg.ctas, blockIdx.x);
+            rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
+            int before = 0;
+            for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+                const int mine = b0 == 0 ? first : tiles_of(b0 + tid), inc = scan(mine);
+                __syncthreads();                                        // warp_tot is read by everyone before it is written again
+                if (lane == 31) sm.warp_tot[warp] = inc;
+                __syncthreads();
+                const int start = before + totals(warp) + inc - mine;
+                if (start <= rg.begin && rg.begin < start + mine) {
+                    sm.b = b0 + tid;
+                    sm.in_seq = rg.begin - start;
+                }
+                before += totals(WARPS);
+                if (before > rg.begin) break;
+            }
+            __syncthreads();
+            rg.b = sm.b;
+            in_seq = sm.in_seq;
+        }
+    }
+    rg.n = rg.item = rg.kt = 0;
+    if (rg.end > rg.begin) {
+        rg.n = paged_len(a, rg.b);
+        const int nt = (rg.n + tile - 1) / tile;
+        rg.item = in_seq / nt;
+        rg.kt = in_seq - rg.item * nt;
     }
     for (int b = blockIdx.x; empty && b < a.B; b += gridDim.x) {
         if (paged_len(a, b) != 0) continue;
@@ -216,13 +234,8 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     // value row are left in shared memory (thread i < 64: key i, thread 64 + i: value i); the tile is requested.  So no step
     // waits for the one it needs, and a request costs a thread one shared-memory read and one add.
     const uint32_t s0 = smem_u32(smem);
-    int lb = rg.b, ln = paged_len(a, lb), lkt, litem;                   // sequence, its keys, tile, item (head * RT + row tile)
-    {
-        const int nt = (ln + kPagedTile - 1) / kPagedTile;
-        litem = (int)(rg.in_seq / nt);
-        lkt = (int)(rg.in_seq - (int64_t)litem * nt);
-    }
-    int64_t lleft = rg.end - rg.begin;                                  // tiles whose table entry is yet to be requested
+    int lb = rg.b, ln = rg.n, lkt = rg.kt, litem = rg.item;             // sequence, its keys, tile, item (head * RT + row tile)
+    int lleft = rg.end - rg.begin;                                      // tiles whose table entry is yet to be requested
     const int64_t page_stride = tid < kPagedTile ? a.pages.k_page : a.pages.v_page;
     const T* const pages = (const T*)(tid < kPagedTile ? a.pages.k : a.pages.v);
     int page = 0, in_page = 0;                                          // of this thread's row in the tile last requested; -1: no such key
@@ -274,8 +287,8 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
             cp_async16(d + SM::TILE_BYTES, reinterpret_cast<const uint8_t*>(vp & ~1ull) + lc * 16, !(vp & 1));
         }
     };
-    const int64_t share = rg.end - rg.begin;
-    int64_t requested = 0;                                              // tiles
+    const int share = rg.end - rg.begin;
+    int requested = 0;                                                  // tiles
     request_entry();
     leave_address(0);
     request_entry();
@@ -299,12 +312,11 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
         kofs[i] = (uint32_t)(((lane & 7) + ((lane >> 4) << 3)) * (HD * 2) + (((2 * i + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
         vofs[i] = (uint32_t)(((lane & 7) + (((lane >> 3) & 1) << 3)) * (HD * 2) + (((2 * i + (lane >> 4)) ^ (lane & 7)) << 4));
     }
-    int b = rg.b, n = paged_len(a, b), nt = (n + kPagedTile - 1) / kPagedTile;
-    int item = (int)(rg.in_seq / nt), kt = (int)(rg.in_seq - (int64_t)item * nt);
+    int b = rg.b, n = rg.n, nt = (n + kPagedTile - 1) / kPagedTile, item = rg.item, kt = rg.kt;
     int stage = 0;
-    for (int64_t left = rg.end - rg.begin; left > 0;) {
+    for (int left = rg.end - rg.begin; left > 0;) {
         const int head = item / RT, row0 = (item - head * RT) * MT;
-        const int kt_first = kt, kt_end = (int)min((int64_t)nt, kt + left);
+        const int kt_first = kt, kt_end = min(nt, kt + left);
         // queries of this warp's 16 rows as operand fragments; rows past R are zeros
         uint32_t qf[KS][4];
 #pragma unroll
@@ -324,10 +336,10 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
         for (; kt < kt_end; ++kt, --left) {
             cp_async_wait<kPagedStages - 2>();
             __syncthreads();                                            // the tile is there, and the stage before it is free
-            if (requested < share) request_tile(stage == 0 ? kPagedStages - 1 : stage - 1, (int)(requested & 1));
+            if (requested < share) request_tile(stage == 0 ? kPagedStages - 1 : stage - 1, requested & 1);
             cp_async_commit();
             ++requested;
-            leave_address((int)(requested & 1));
+            leave_address(requested & 1);
             request_entry();
             const uint32_t sk = s0 + stage * SM::STAGE_BYTES + wk * KW * (HD * 2), sv = sk + SM::TILE_BYTES;
             if (++stage == kPagedStages) stage = 0;
@@ -476,7 +488,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
         }
         if (begins && !ends && tid == 0) {
             // tiles of the line from the item's first to its last; the next CTAs have the rest of them
-            const int64_t last = rg.end + (nt - kt_end) - 1;
+            const int last = rg.end + (nt - kt_end) - 1;
             a.desc[blockIdx.x] = make_int4(b, item, paged_owner(rg.total, rg.ctas, last) - (int)blockIdx.x + 1, 0);
         }
         // next item
@@ -490,65 +502,77 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     cp_async_wait<0>();
 }
 
-// Joins the parts of the items that several CTAs worked on.  blockIdx.x: the CTA in which an item begins; blockIdx.y: ROWS of its
-// rows, 4 / ROWS warps to a row, each warp a share of the parts, a lane HD / 32 columns.
-template <typename T, int HD, int ROWS>
+// Joins the parts of the items that several CTAs worked on.  blockIdx.x: the CTA in which an item begins.  WPR warps share a row (a part
+// of the parts each, where an item may be in many of them); otherwise a warp has RPW rows, whose requests are in flight together.
+template <typename T, int HD, int WPR, int RPW>
 __global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedArgs a, int MT) {
     grid_launch_dependents();
     grid_dependency_wait();
-    constexpr int E = HD / 32, WPR = 4 / ROWS;
-    __shared__ float so[4][HD];
+    constexpr int E = HD / 32;                                          // columns of a lane
+    __shared__ float so[WPR > 1 ? 4 : 1][HD];
     __shared__ float2 sml[4];
     const int4 d = a.desc[blockIdx.x];
     if (d.z == 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int R = a.T * a.group, RT = (R + MT - 1) / MT;
-    const int head = d.y / RT, row0 = (d.y - head * RT) * MT, r = blockIdx.y * ROWS + warp / WPR;
-    const bool real = r < MT && row0 + r < R;
-    float m = -INFINITY, l = 0.f, o[E] = {};
-    if (real) {
+    const int R = a.T * a.group, RT = (R + MT - 1) / MT, head = d.y / RT, row0 = (d.y - head * RT) * MT;
+    const int r0 = (blockIdx.y * (4 / WPR) + warp / WPR) * RPW, rows = min(min(MT, R - row0) - r0, RPW);
+    if (WPR == 1 && rows <= 0) return;
+    float m[RPW], l[RPW], o[RPW][E];
+#pragma unroll
+    for (int i = 0; i < RPW; ++i) {
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[i][e] = 0.f;
+    }
 #pragma unroll 4
-        for (int f = warp % WPR; f < d.z; f += WPR) {
-            const int64_t slot = f == 0 ? (int64_t)blockIdx.x * 2 + 1 : (int64_t)(blockIdx.x + f) * 2;
-            const float2 p = a.partial_ml[slot * MT + r];
+    for (int f = warp % WPR; f < d.z; f += WPR) {
+        const int64_t slot = f == 0 ? (int64_t)blockIdx.x * 2 + 1 : (int64_t)(blockIdx.x + f) * 2, at = slot * MT + r0;
+#pragma unroll
+        for (int i = 0; i < RPW; ++i) {
+            if (i >= rows) break;
+            const float2 p = a.partial_ml[at + i];
             float x[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = a.partial[(slot * MT + r) * HD + lane * E + e];
-            const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
-            const float fo = ex2_approx(m - base), fn = ex2_approx(p.x - base);
-            m = top;
-            l = l * fo + p.y * fn;
+            for (int e = 0; e < E; e += 2) *reinterpret_cast<float2*>(x + e) = *reinterpret_cast<const float2*>(a.partial + (at + i) * HD + lane * E + e);
+            const float top = fmaxf(m[i], p.x), base = top == -INFINITY ? 0.f : top;
+            const float fo = ex2_approx(m[i] - base), fn = ex2_approx(p.x - base);
+            m[i] = top;
+            l[i] = l[i] * fo + p.y * fn;
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = o[e] * fo + x[e] * fn;
+            for (int e = 0; e < E; ++e) o[i][e] = o[i][e] * fo + x[e] * fn;
         }
     }
     if (WPR > 1) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) so[warp][lane * E + e] = o[e];
-        if (lane == 0) sml[warp] = make_float2(m, l);
+        for (int e = 0; e < E; ++e) so[warp][lane * E + e] = o[0][e];
+        if (lane == 0) sml[warp] = make_float2(m[0], l[0]);
         __syncthreads();
         if (warp != 0) return;
-        m = -INFINITY;
-        l = 0.f;
+        m[0] = -INFINITY;
+        l[0] = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, sml[w].x);
+        for (int w = 0; w < 4; ++w) m[0] = fmaxf(m[0], sml[w].x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.f;
+        for (int e = 0; e < E; ++e) o[0][e] = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float f = m == -INFINITY ? 1.f : ex2_approx(sml[w].x - m);
-            l += sml[w].y * f;
+            const float f = m[0] == -INFINITY ? 1.f : ex2_approx(sml[w].x - m[0]);
+            l[0] += sml[w].y * f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] += so[w][lane * E + e] * f;
+            for (int e = 0; e < E; ++e) o[0][e] += so[w][lane * E + e] * f;
         }
     }
-    if (!real) return;
-    const float inv = 1.f / l;
-    const int rr = row0 + r, t = rr / a.group, gq = rr - t * a.group;
-    T* out = (T*)a.out + d.x * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + lane * E;
 #pragma unroll
-    for (int e = 0; e < E; e += 2) *reinterpret_cast<typename Pack2<T>::type*>(out + e) = Pack2<T>::down(o[e] * inv, o[e + 1] * inv);
-    if (lane == 0 && a.lse) a.lse[((int64_t)d.x * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(l)) * 0.69314718055994531f;
+    for (int i = 0; i < RPW; ++i) {
+        if (i >= rows) break;
+        const float inv = 1.f / l[i];
+        const int rr = row0 + r0 + i, t = rr / a.group, gq = rr - t * a.group;
+        T* out = (T*)a.out + d.x * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) *reinterpret_cast<typename Pack2<T>::type*>(out + e) = Pack2<T>::down(o[i][e] * inv, o[i][e + 1] * inv);
+        if (lane == 0 && a.lse) a.lse[((int64_t)d.x * a.T + t) * a.nq + head * a.group + gq] = (m[i] + log2f(l[i])) * 0.69314718055994531f;
+    }
 }
 
 }  // namespace jot

@@ -74,15 +74,15 @@ __host__ __device__ constexpr uint32_t umma_idesc16(int M, int N, bool b_mn_majo
 // The parts of items a CTA's share consists of, in order.
 struct PagedWalk {
     int b, n, nt, item, kt, cnt;          // sequence, its keys and tiles, item, first tile and number of tiles of this part
-    int64_t left;                         // tiles of the share from this part on
-    __device__ __forceinline__ PagedWalk(const PagedArgs& a, const PagedRange& rg, int tile) {
+    int left;                             // tiles of the share from this part on
+    __device__ __forceinline__ PagedWalk(const PagedRange& rg, int tile) {
         b = rg.b;
-        n = paged_len(a, b);
+        n = rg.n;
         nt = (n + tile - 1) / tile;
-        item = (int)(rg.in_seq / nt);
-        kt = (int)(rg.in_seq - (int64_t)item * nt);
+        item = rg.item;
+        kt = rg.kt;
         left = rg.end - rg.begin;
-        cnt = (int)min((int64_t)(nt - kt), left);
+        cnt = min(nt - kt, left);
     }
     __device__ __forceinline__ bool next(const PagedArgs& a, int per_b, int tile) {
         left -= cnt;
@@ -93,7 +93,7 @@ struct PagedWalk {
             do { ++b; n = paged_len(a, b); } while (n <= 0);
             nt = (n + tile - 1) / tile;
         }
-        cnt = (int)min((int64_t)nt, left);
+        cnt = min(nt, left);
         return true;
     }
 };
@@ -133,7 +133,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], Role::QUERY_WARPS * 32);
-            mbar_init(&q_empty[i], TWO ? 2 : 10);          // both streams' products; the softmax warps, which use the room at the end of a part
+            mbar_init(&q_empty[i], 10);          // both streams' products; the softmax warps, which use the room at the end of a part
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
             mbar_init(&pv_done[i], 1);
@@ -185,7 +185,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         if (TMA && warp == Role::PROD) {
             // ================================ producer by TMA: lane = page of the tile ================================
             const int ps = a.pages.page_size, boxes = ps <= 128 ? KEYS / ps : 1, box = min(ps, 128);
-            PagedWalk w(a, rg, KEYS);
+            PagedWalk w(rg, KEYS);
             PagedWalk ahead = w;                                   // the tile whose page entry is requested next
             int ahead_j = 0;
             bool ahead_more = true;
@@ -277,13 +277,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 return w;
             };
             // page entries two tiles ahead, addresses one
-            int lb = rg.b, ln = paged_len(a, lb), lkt, litem;
-            {
-                const int nt = (ln + TILE - 1) / TILE;
-                litem = (int)(rg.in_seq / nt);
-                lkt = (int)(rg.in_seq - (int64_t)litem * nt);
-            }
-            int64_t lleft = rg.end - rg.begin;
+            int lb = rg.b, ln = rg.n, lkt = rg.kt, litem = rg.item, lleft = rg.end - rg.begin;
             int page = 0, in_page = 0;
             bool exists = false;
             auto request_entry = [&]() {
@@ -320,7 +314,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 row_at[buf][pt] = ka;
                 row_at[buf][TILE + pt] = va;
             };
-            PagedWalk w(a, rg, KEYS);
+            PagedWalk w(rg, KEYS);
             if (!TMA) {
                 request_entry();
                 leave_address(0);
@@ -369,7 +363,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
             const bool elected = elect_one();
             const uint64_t qd0 = umma_desc_k128(sQ) + (uint64_t)(TWO ? s * (SM::TILE_BYTES >> 4) : 0), kd0 = umma_desc_k128(sK), vd0 = umma_desc_mn128(sV);
             const uint32_t d_s = tmem_base + s * 128, d_o = tmem_base + O_COL + s * 128;
-            PagedWalk w(a, rg, KEYS);
+            PagedWalk w(rg, KEYS);
             uint32_t part = 0, used = 0, made = 0, done = 0, tails = 0;        // parts, those with a tile of this stream, first and second products, tails so far
             bool ok = true, more = true;
             for (; ok && more; ++part) {
@@ -458,7 +452,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
             const int rep = TWO ? 0 : r128 / ROWS, wr = TWO ? s * 128 + quad * 32 : quad * 32 % ROWS;      // copy of the row; first row of the warp
             const uint32_t lanes = tmem_base + (uint32_t(quad * 32) << 16), sc = lanes + s * 128;
             const float c = a.scale_log2, none = c < 0.f ? INFINITY : -INFINITY;
-            PagedWalk w(a, rg, KEYS);
+            PagedWalk w(rg, KEYS);
             uint32_t done[2] = {0, 0}, part = 0, g_ph = 0;         // tiles of each stream so far
             bool ok = true, more = true;
             for (; ok && more; ++part) {
@@ -580,161 +574,117 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 // ---- the part goes out ----
                 const bool begins = w.kt == 0, whole = begins && w.cnt == w.nt;
                 const int64_t slot = (int64_t)blockIdx.x * 2 + (begins ? 1 : 0);
-                // rt: row within the item; 32 columns of it: x
-                auto put = [&](int rt, int col, const float* x, int count) {
-                    const int r = row0 + rt, t = r / a.group, gq = r - t * a.group;
-                    if (whole) {
-                        T* dst = (T*)a.out + w.b * a.o_b + t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + col;
-                        if (count == 4) {
-                            typename Pack2<T>::type lo = Pack2<T>::down(x[0], x[1]), hi = Pack2<T>::down(x[2], x[3]);
-                            *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < count / 8; ++e) reinterpret_cast<uint4*>(dst)[e] = pack8<T>(x + 8 * e);
-                        }
-                    } else {
-                        float4* dst = reinterpret_cast<float4*>(a.partial + (slot * MT + rt) * HD + col);
-#pragma unroll
-                        for (int e = 0; e < count / 4; ++e) dst[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
-                    }
-                };
-                auto put_ml = [&](int rt, float m, float sum) {
-                    const int r = row0 + rt, t = r / a.group, gq = r - t * a.group;
-                    if (!whole) a.partial_ml[slot * MT + rt] = make_float2(m, sum);
-                    else if (a.lse) a.lse[((int64_t)w.b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(sum)) * 0.69314718055994531f;
-                };
+                // Each thread weighs what its lane holds of a row, and the rows leave through the room of the part's queries, which are used up: whole
+                // rows of 16-byte chunks (chunk e of row r at e ^ (r mod 8)), and copies of a row are added up on the way.  With ROWS <= 128 the
+                // streams meet here, too: a warpgroup has half of the columns of both accumulators.
+                constexpr int COLS = TWO ? HD : HD / 2, ROUND = COLS / 2, CH4 = ROUND / 4, SWZ = CH4 < 8 ? CH4 - 1 : 7;
+                constexpr int OWN = TWO ? 128 : ROWS, ITEMS = OWN * CH4 / 128;         // rows of the warpgroup; chunks of a round a thread takes
+                const int col0 = TWO ? 0 : s * COLS, base0 = TWO ? s * 128 : 0;
+                const bool both = !TWO && w.cnt > 1;
+                float wa = 1.f, wb = 0.f, m = mc, sum = l;
                 if (TWO) {
-                    // thread = row
-                    if (!(ok = wait_all(&pv_done[s], (done[s] - 1) & 1))) break;
-                    const int rt = s * 128 + r128;
-                    const bool real = row0 + rt < R;
-                    if (!idle) {
-                        tc_fence_after();
-                        const float weight = whole ? 1.f / l : 1.f;
-#pragma unroll
-                        for (int ch = 0; ch < HD / 32; ++ch) {
-                            float o[32];
-                            tmem_ld32(lanes + O_COL + s * 128 + ch * 32, o);
-                            tmem_ld_wait_regs(o);
-#pragma unroll
-                            for (int x = 0; x < 32; ++x) o[x] *= weight;
-                            if (real) put(rt, ch * 32, o, 32);
-                        }
-                        if (real) put_ml(rt, mc, l);
-                        tc_fence_before();
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&o_empty[s]);
+                    ok = wait_all(&pv_done[s], (done[s] - 1) & 1);
                 } else {
-                    // The streams and the copies of a row meet: each thread weighs what its lane holds in both accumulators, half of the columns
-                    // a warpgroup, and the copies are added up through the room of this part's queries, which are used up.
                     x_ml[part & 1][s][r128] = make_float2(mc, l);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&x_bar);
                     ok = wait_all(&x_bar, part & 1);
                     if (ok) ok = wait_all(&pv_done[0], (done[0] - 1) & 1);
-                    if (ok && w.cnt > 1) ok = wait_all(&pv_done[1], (done[1] - 1) & 1);
-                    if (!ok) break;
-                    const bool both = w.cnt > 1;
-                    auto meet = [&](int rt, float& m, float& sum) {            // maximum and sum over everything that has keys of row rt
-                        m = -INFINITY;
-                        sum = 0.f;
+                    if (ok && both) ok = wait_all(&pv_done[1], (done[1] - 1) & 1);
+                    // maximum and sum over everything that has keys of the row
+                    const int rt = r128 % ROWS;
+                    m = -INFINITY;
+                    sum = 0.f;
 #pragma unroll
-                        for (int q = 0; q < REP; ++q) {
-                            m = fmaxf(m, x_ml[part & 1][0][q * ROWS + rt].x);
-                            if (both) m = fmaxf(m, x_ml[part & 1][1][q * ROWS + rt].x);
-                        }
-#pragma unroll
-                        for (int q = 0; q < REP; ++q) {
-                            const float2 x0 = x_ml[part & 1][0][q * ROWS + rt], x1 = x_ml[part & 1][1][q * ROWS + rt];
-                            sum += x0.y * (m == -INFINITY ? 1.f : ex2_approx(x0.x - m));
-                            if (both) sum += x1.y * (m == -INFINITY ? 1.f : ex2_approx(x1.x - m));
-                        }
-                    };
-                    float* room = reinterpret_cast<float*>(smem + (part & 1) * SM::TILE_BYTES + s * (SM::TILE_BYTES / 2));
-                    constexpr int ROUND = HD / 4, ROUNDS = 2, CH4 = ROUND / 4;       // columns of a round, 16-byte chunks of them
-                    float wa = 0.f, wb = 0.f;
-                    if (!idle) {
-                        float m, sum;
-                        const int rt = r128 % ROWS;
-                        meet(rt, m, sum);
-                        wa = m == -INFINITY ? 1.f : ex2_approx(x_ml[part & 1][0][r128].x - m);
-                        wb = m == -INFINITY ? 1.f : ex2_approx(x_ml[part & 1][1][r128].x - m);
-                        tc_fence_after();
+                    for (int q = 0; q < REP; ++q) {
+                        m = fmaxf(m, x_ml[part & 1][0][q * ROWS + rt].x);
+                        if (both) m = fmaxf(m, x_ml[part & 1][1][q * ROWS + rt].x);
                     }
+                    const float mb = m == -INFINITY ? 0.f : m;                 // (no finite score at all: sums are 0 or NaN)
 #pragma unroll
-                    for (int round = 0; round < ROUNDS; ++round) {
-                        const int col = s * (HD / 2) + round * ROUND;
-                        if (!idle) {
-                            float o[32], o2[32];
-                            if (ROUND == 32) {
-                                tmem_ld32(lanes + O_COL + col, o);
-                                if (both) tmem_ld32(lanes + O_COL + 128 + col, o2);
-                                tmem_ld_wait_regs(o);
-                                if (both) tmem_ld_wait_regs(o2);
-                            } else {
+                    for (int q = 0; q < REP; ++q) {
+                        const float2 x0 = x_ml[part & 1][0][q * ROWS + rt], x1 = x_ml[part & 1][1][q * ROWS + rt];
+                        sum += x0.y * (m == -INFINITY ? 1.f : ex2_approx(x0.x - mb));
+                        if (both) sum += x1.y * (m == -INFINITY ? 1.f : ex2_approx(x1.x - mb));
+                    }
+                    wa = m == -INFINITY ? 1.f : ex2_approx(x_ml[part & 1][0][r128].x - mb);
+                    wb = m == -INFINITY ? 1.f : ex2_approx(x_ml[part & 1][1][r128].x - mb);
+                }
+                if (!ok) break;
+                if (whole) {
+                    const float inv = 1.f / sum;
+                    wa *= inv;
+                    wb *= inv;
+                }
+                float* const room = reinterpret_cast<float*>(smem + (TWO ? s * SM::TILE_BYTES : (part & 1) * SM::TILE_BYTES + s * (SM::TILE_BYTES / 2)));
+                if (!idle) tc_fence_after();
 #pragma unroll
-                                for (int e = 0; e < ROUND / 8; ++e) {
-                                    tmem_ld8(lanes + O_COL + col + 8 * e, o + 8 * e);
-                                    if (both) tmem_ld8(lanes + O_COL + 128 + col + 8 * e, o2 + 8 * e);
-                                }
+                for (int round = 0; round < 2; ++round) {
+                    if (!idle) {
 #pragma unroll
-                                for (int e = 0; e < ROUND / 8; ++e) {
-                                    tmem_ld8_wait(o + 8 * e);
-                                    if (both) tmem_ld8_wait(o2 + 8 * e);
-                                }
-                            }
+                        for (int c0 = 0; c0 < ROUND; c0 += 16) {
+                            float o[16], o2[16];
+                            tmem_ld16(lanes + O_COL + (TWO ? s * 128 : 0) + col0 + round * ROUND + c0, o);
+                            if (both) tmem_ld16(lanes + O_COL + 128 + col0 + round * ROUND + c0, o2);
+                            tmem_ld16_wait(o);
+                            if (both) tmem_ld16_wait(o2);
 #pragma unroll
-                            for (int x = 0; x < ROUND; ++x) o[x] = both ? o[x] * wa + o2[x] * wb : o[x] * wa;
+                            for (int x = 0; x < 16; ++x) o[x] = both ? o[x] * wa + o2[x] * wb : o[x] * wa;
 #pragma unroll
-                            for (int e = 0; e < CH4; ++e)
-                                reinterpret_cast<float4*>(room + r128 * ROUND)[e ^ (lane & (CH4 - 1))] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                            for (int e = 0; e < 4; ++e)
+                                reinterpret_cast<float4*>(room + r128 * ROUND)[(c0 / 4 + e) ^ (lane & SWZ)] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                         }
-                        if (round == ROUNDS - 1) {
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) {
-                                mbar_arrive(&o_empty[0]);
-                                if (both) mbar_arrive(&o_empty[1]);
-                            }
-                        }
-                        // the warpgroup's rows are in the room
+                    }
+                    if (round == 1) {
+                        tc_fence_before();
                         __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(&o_empty[TWO ? s : 0]);
+                            if (both) mbar_arrive(&o_empty[1]);
+                        }
+                    }
+                    // the warpgroup's rows are in the room
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&g_bar[s]);
+                    if (!(ok = wait_all(&g_bar[s], g_ph))) break;
+                    g_ph ^= 1;
+#pragma unroll 2
+                    for (int k = 0; k < ITEMS; ++k) {
+                        const int i = k * 128 + (tid & 127), rt = i / CH4, e = i % CH4, r = row0 + base0 + rt;
+                        if (r >= R) break;
+                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int q = 0; q < REP; ++q) {
+                            const float4 y = reinterpret_cast<const float4*>(room + (q * ROWS + rt) * ROUND)[e ^ (rt & SWZ)];
+                            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                        }
+                        const int col = col0 + round * ROUND + 4 * e;
+                        if (whole) {
+                            const int t = r / a.group, gq = r - t * a.group;
+                            typename Pack2<T>::type lo = Pack2<T>::down(x.x, x.y), hi = Pack2<T>::down(x.z, x.w);
+                            *reinterpret_cast<uint2*>((T*)a.out + w.b * a.o_b + t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + col) =
+                                make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+                        } else {
+                            *reinterpret_cast<float4*>(a.partial + (slot * MT + base0 + rt) * HD + col) = x;
+                        }
+                    }
+                    __syncwarp();
+                    if (round == 0) {
                         if (lane == 0) mbar_arrive(&g_bar[s]);
                         if (!(ok = wait_all(&g_bar[s], g_ph))) break;
                         g_ph ^= 1;
-                        for (int i = tid & 127; i < min(ROWS, R - row0) * CH4; i += 128) {
-                            const int rt = i / CH4, e = i % CH4;
-                            float x[4] = {};
-#pragma unroll
-                            for (int q = 0; q < REP; ++q) {
-                                const int rr = q * ROWS + rt;
-                                const float4 y = reinterpret_cast<const float4*>(room + rr * ROUND)[e ^ (rr & (CH4 - 1))];
-                                x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w;
-                            }
-                            float m, sum;
-                            meet(rt, m, sum);
-                            if (whole) {
-                                const float inv = 1.f / sum;
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) x[k] *= inv;
-                            }
-                            put(rt, col + 4 * e, x, 4);
-                            if (s == 0 && round == 0 && e == 0) put_ml(rt, m, sum);
-                        }
-                        __syncwarp();
-                        if (round + 1 < ROUNDS) {
-                            if (lane == 0) mbar_arrive(&g_bar[s]);
-                            if (!(ok = wait_all(&g_bar[s], g_ph))) break;
-                            g_ph ^= 1;
-                        }
                     }
-                    if (!ok) break;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&q_empty[part & 1]);
+                }
+                if (!ok) break;
+                if (lane == 0) mbar_arrive(&q_empty[TWO ? 0 : part & 1]);
+                // (of the copies of a row, the first)
+                if (r128 < OWN && (TWO || s == 0) && row0 + base0 + r128 < R) {
+                    const int r = row0 + base0 + r128, t = r / a.group, gq = r - t * a.group;
+                    if (!whole) a.partial_ml[slot * MT + base0 + r128] = make_float2(m, sum);
+                    else if (a.lse) a.lse[((int64_t)w.b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(sum)) * 0.69314718055994531f;
                 }
                 if (begins && !whole && tid == 0) {
-                    const int64_t last = rg.end + (w.nt - w.cnt) - 1;
+                    const int last = rg.end + (w.nt - w.cnt) - 1;
                     a.desc[blockIdx.x] = make_int4(w.b, w.item, paged_owner(rg.total, rg.ctas, last) - (int)blockIdx.x + 1, 0);
                 }
                 more = w.next(a, per_b, KEYS);
