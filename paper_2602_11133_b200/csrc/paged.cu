@@ -105,7 +105,7 @@ struct PagedSpace {
     size_t desc, ml, partial, total;
 };
 PagedSpace paged_space(int row_tile, int head_dim) {
-    const size_t ctas = row_tile == 16 ? kPagedMaxCtas : kUmmaPagedMaxCtas;
+    const size_t ctas = row_tile == 16 ? kPagedMaxCtas : (row_tile == 256 ? kUmmaPagedMaxCtas : 2 * kUmmaPagedMaxCtas);      // or streams of CTAs
     PagedSpace s;
     s.desc = 0;
     s.ml = align_up(ctas * sizeof(int4), 256);
@@ -114,15 +114,13 @@ PagedSpace paged_space(int row_tile, int head_dim) {
     return s;
 }
 
-// The second kernel: four warps to a row where an item may be in many parts (few items on many CTAs), else a warp to a row, or to
-// four where there are many rows (their requests are in flight together: 224 rows of eight sequences, 20 MB of parts).
+// The second kernel: four warps to a row where an item may be in many parts (few items on many CTAs), else a warp to a row.
 template <typename T, int HD>
 int launch_join(const PagedArgs& a, int grid, int row_tile, cudaStream_t st) {
     const int all = a.T * a.group, rows = std::min(row_tile, all), row_tiles = (all + row_tile - 1) / row_tile;
     auto go = [&](auto* kernel, int per_cta) { launch_k(kernel, dim3((unsigned)grid, (unsigned)((rows + per_cta - 1) / per_cta)), dim3(kPagedThreads), 0, st, a, row_tile); };
-    if (grid > 8ll * a.B * a.nkv * row_tiles) go(paged_join_kernel<T, HD, 4, 1>, 1);
-    else if (rows <= 32) go(paged_join_kernel<T, HD, 1, 1>, 4);
-    else go(paged_join_kernel<T, HD, 1, 4>, 16);
+    if (grid > 8ll * a.B * a.nkv * row_tiles) go(paged_join_kernel<T, HD, 4>, 1);
+    else go(paged_join_kernel<T, HD, 1>, 4);
     return launch_check();
 }
 
@@ -192,7 +190,7 @@ int launch_paged_umma_t(const DeviceInfo* di, const PagedArgs& a, int grid, cuda
         std::memset(&mk, 0, sizeof(mk));
         mv = mk;
     }
-    launch_k(kernel, dim3((unsigned)grid), dim3(UmmaPagedRoles<TMA>::THREADS), smem, st, a, mk, mv);
+    launch_k(kernel, dim3((unsigned)grid), dim3(UmmaPagedRoles<ROWS, TMA>::THREADS), smem, st, a, mk, mv);
     return launch_check();
 }
 
@@ -200,10 +198,11 @@ template <typename T, int HD, int ROWS>
 int launch_paged_umma(const DeviceInfo* di, const PagedArgs& a, int64_t items, cudaStream_t st) {
     const bool tma = paged_tma_pages(a.pages.page_size) && a.pages.k_page >= 0 && a.pages.v_page >= 0;
     const int64_t tiles = paged_tiles(a, tma ? paged_tma_keys(a.pages.page_size) : kUmmaPagedTile);
-    const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(di->sms, kUmmaPagedMaxCtas));
+    constexpr int streams = ROWS == 256 ? 1 : 2;
+    const int grid = (int)std::min<int64_t>((paged_most(a, items, tiles) + streams - 1) / streams, std::min(di->sms, kUmmaPagedMaxCtas));
     if (tma) JOT_TRY((launch_paged_umma_t<T, HD, ROWS, true>(di, a, grid, st)));
     else JOT_TRY((launch_paged_umma_t<T, HD, ROWS, false>(di, a, grid, st)));
-    return tiles <= 1 ? JOT_OK : launch_join<T, HD>(a, grid, ROWS, st);
+    return tiles <= 1 ? JOT_OK : launch_join<T, HD>(a, grid * streams, ROWS, st);
 }
 
 template <typename T, int HD>

@@ -93,7 +93,7 @@ __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) {
 // The share of a CTA on the line of tiles (fewer than 2^31, which the host makes sure of), and where it begins.
 struct PagedRange {
     int begin, end, total;          // tiles of the line
-    int ctas;                       // CTAs that have a share
+    int ctas;                       // CTAs, or streams of CTAs, that have a share
     int b, n, item, kt;             // sequence of the first tile, its keys; item within the sequence; tile within the item
 };
 
@@ -105,13 +105,14 @@ __host__ __device__ __forceinline__ int paged_owner(int total, int ctas, int t) 
 }
 
 struct PagedRangeSmem {
-    int warp_tot[16], b, in_seq;
+    int warp_tot[16], b[2], in_seq[2];
 };
 
-// The share of this CTA on the line of tiles of `tile` keys, per_b items a sequence; sequences without a key are answered here:
-// zeros, and the logarithm of nothing.  All THREADS threads of the CTA call it; lens is read after the preceding kernel's end.
-template <typename T, int HD, int THREADS>
-__device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, int per_b, PagedRangeSmem& sm) {
+// The line of tiles of `tile` keys, per_b items a sequence, and the share of it that this thread's stream has: stream `mine` of the
+// STREAMS that each CTA runs.  Sequences without a key are answered here: zeros, and the logarithm of nothing.  All THREADS threads of
+// the CTA call it; lens is read after the preceding kernel's end.
+template <typename T, int HD, int THREADS, int STREAMS>
+__device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, int per_b, int mine, PagedRangeSmem& sm) {
     constexpr int WARPS = THREADS / 32, CPR = HD / 8;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     bool empty = false;             // whether a sequence of this thread has no key
@@ -133,15 +134,19 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
     PagedRange rg;
     int in_seq = 0;
     const int first = tiles_of(a.B <= 32 ? lane : tid);
+    auto cut = [&](int stream, int& begin, int& end) {
+        const int i = blockIdx.x * STREAMS + stream;
+        begin = i < rg.ctas ? paged_share(rg.total, rg.ctas, i) : 0;
+        end = i < rg.ctas ? paged_share(rg.total, rg.ctas, i + 1) : 0;
+    };
+    rg.b = 0;
     if (a.B <= 32) {                // every warp for itself
         const int inc = scan(first);
         rg.total = __shfl_sync(0xffffffffu, inc, 31);
-        rg.ctas = min((int)gridDim.x, rg.total);
+        rg.ctas = min((int)gridDim.x * STREAMS, rg.total);
         empty = __any_sync(0xffffffffu, empty);
-        rg.begin = rg.end = rg.b = 0;
-        if ((int)blockIdx.x < rg.ctas) {
-            rg.begin = paged_share(rg.total, rg.ctas, blockIdx.x);
-            rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
+        cut(mine, rg.begin, rg.end);
+        if (rg.end > rg.begin) {
             rg.b = __popc(__ballot_sync(0xffffffffu, inc <= rg.begin));        // sequences that end before it
             in_seq = rg.begin - __shfl_sync(0xffffffffu, inc - first, rg.b);
         }
@@ -157,28 +162,30 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
             return t;
         };
         rg.total = totals(WARPS);
-        rg.ctas = min((int)gridDim.x, rg.total);
-        rg.begin = rg.end = rg.b = 0;
-        if ((int)blockIdx.x < rg.ctas) {
-            rg.begin = paged_share(rg.total, rg.ctas, blockIdx.x);
-            rg.end = paged_share(rg.total, rg.ctas, blockIdx.x + 1);
-            int before = 0;
-            for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-                const int mine = b0 == 0 ? first : tiles_of(b0 + tid), inc = scan(mine);
-                __syncthreads();                                        // warp_tot is read by everyone before it is written again
-                if (lane == 31) sm.warp_tot[warp] = inc;
-                __syncthreads();
-                const int start = before + totals(warp) + inc - mine;
-                if (start <= rg.begin && rg.begin < start + mine) {
-                    sm.b = b0 + tid;
-                    sm.in_seq = rg.begin - start;
-                }
-                before += totals(WARPS);
-                if (before > rg.begin) break;
-            }
+        rg.ctas = min((int)gridDim.x * STREAMS, rg.total);
+        cut(mine, rg.begin, rg.end);
+        int before = 0;
+        for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+            const int tiles = b0 == 0 ? first : tiles_of(b0 + tid), inc = scan(tiles);
+            __syncthreads();                                        // warp_tot is read by everyone before it is written again
+            if (lane == 31) sm.warp_tot[warp] = inc;
             __syncthreads();
-            rg.b = sm.b;
-            in_seq = sm.in_seq;
+            const int start = before + totals(warp) + inc - tiles;
+#pragma unroll
+            for (int i = 0; i < STREAMS; ++i) {
+                int begin, end;
+                cut(i, begin, end);
+                if (start <= begin && begin < start + tiles && begin < end) {
+                    sm.b[i] = b0 + tid;
+                    sm.in_seq[i] = begin - start;
+                }
+            }
+            before += totals(WARPS);
+        }
+        __syncthreads();
+        if (rg.end > rg.begin) {
+            rg.b = sm.b[mine];
+            in_seq = sm.in_seq[mine];
         }
     }
     rg.n = rg.item = rg.kt = 0;
@@ -225,7 +232,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     const int R = a.T * a.group, RT = (R + MT - 1) / MT;
     const int per_b = a.nkv * RT;                                       // items of a sequence
 
-    const PagedRange rg = paged_range<T, HD, kPagedThreads>(a, kPagedTile, per_b, range_smem);
+    const PagedRange rg = paged_range<T, HD, kPagedThreads, 1>(a, kPagedTile, per_b, 0, range_smem);
     if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if ((int)blockIdx.x >= rg.ctas) return;
 
@@ -502,77 +509,62 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     cp_async_wait<0>();
 }
 
-// Joins the parts of the items that several CTAs worked on.  blockIdx.x: the CTA in which an item begins.  WPR warps share a row (a part
-// of the parts each, where an item may be in many of them); otherwise a warp has RPW rows, whose requests are in flight together.
-template <typename T, int HD, int WPR, int RPW>
+// Joins the parts of the items that several CTAs worked on.  blockIdx.x: the CTA in which an item begins; WPR warps share a row, a part
+// of the parts each, a lane HD / 32 columns.
+template <typename T, int HD, int WPR>
 __global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedArgs a, int MT) {
     grid_launch_dependents();
     grid_dependency_wait();
-    constexpr int E = HD / 32;                                          // columns of a lane
+    constexpr int E = HD / 32;
     __shared__ float so[WPR > 1 ? 4 : 1][HD];
     __shared__ float2 sml[4];
     const int4 d = a.desc[blockIdx.x];
     if (d.z == 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int R = a.T * a.group, RT = (R + MT - 1) / MT, head = d.y / RT, row0 = (d.y - head * RT) * MT;
-    const int r0 = (blockIdx.y * (4 / WPR) + warp / WPR) * RPW, rows = min(min(MT, R - row0) - r0, RPW);
-    if (WPR == 1 && rows <= 0) return;
-    float m[RPW], l[RPW], o[RPW][E];
-#pragma unroll
-    for (int i = 0; i < RPW; ++i) {
-        m[i] = -INFINITY;
-        l[i] = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[i][e] = 0.f;
-    }
+    const int r = blockIdx.y * (4 / WPR) + warp / WPR;
+    if (r >= min(MT, R - row0)) return;                                 // (with WPR = 4 all of the CTA's warps have this row)
+    float m = -INFINITY, l = 0.f, o[E] = {};
 #pragma unroll 4
     for (int f = warp % WPR; f < d.z; f += WPR) {
-        const int64_t slot = f == 0 ? (int64_t)blockIdx.x * 2 + 1 : (int64_t)(blockIdx.x + f) * 2, at = slot * MT + r0;
+        const int64_t at = (f == 0 ? (int64_t)blockIdx.x * 2 + 1 : (int64_t)(blockIdx.x + f) * 2) * MT + r;
+        const float2 p = a.partial_ml[at];
+        float x[E];
 #pragma unroll
-        for (int i = 0; i < RPW; ++i) {
-            if (i >= rows) break;
-            const float2 p = a.partial_ml[at + i];
-            float x[E];
+        for (int e = 0; e < E; e += 2) *reinterpret_cast<float2*>(x + e) = *reinterpret_cast<const float2*>(a.partial + at * HD + lane * E + e);
+        const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
+        const float fo = ex2_approx(m - base), fn = ex2_approx(p.x - base);
+        m = top;
+        l = l * fo + p.y * fn;
 #pragma unroll
-            for (int e = 0; e < E; e += 2) *reinterpret_cast<float2*>(x + e) = *reinterpret_cast<const float2*>(a.partial + (at + i) * HD + lane * E + e);
-            const float top = fmaxf(m[i], p.x), base = top == -INFINITY ? 0.f : top;
-            const float fo = ex2_approx(m[i] - base), fn = ex2_approx(p.x - base);
-            m[i] = top;
-            l[i] = l[i] * fo + p.y * fn;
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[i][e] = o[i][e] * fo + x[e] * fn;
-        }
+        for (int e = 0; e < E; ++e) o[e] = o[e] * fo + x[e] * fn;
     }
     if (WPR > 1) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) so[warp][lane * E + e] = o[0][e];
-        if (lane == 0) sml[warp] = make_float2(m[0], l[0]);
+        for (int e = 0; e < E; ++e) so[warp][lane * E + e] = o[e];
+        if (lane == 0) sml[warp] = make_float2(m, l);
         __syncthreads();
         if (warp != 0) return;
-        m[0] = -INFINITY;
-        l[0] = 0.f;
+        m = -INFINITY;
+        l = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m[0] = fmaxf(m[0], sml[w].x);
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, sml[w].x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[0][e] = 0.f;
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float f = m[0] == -INFINITY ? 1.f : ex2_approx(sml[w].x - m[0]);
-            l[0] += sml[w].y * f;
+            const float f = m == -INFINITY ? 1.f : ex2_approx(sml[w].x - m);
+            l += sml[w].y * f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[0][e] += so[w][lane * E + e] * f;
+            for (int e = 0; e < E; ++e) o[e] += so[w][lane * E + e] * f;
         }
     }
+    const float inv = 1.f / l;
+    const int rr = row0 + r, t = rr / a.group, gq = rr - t * a.group;
+    T* out = (T*)a.out + d.x * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + lane * E;
 #pragma unroll
-    for (int i = 0; i < RPW; ++i) {
-        if (i >= rows) break;
-        const float inv = 1.f / l[i];
-        const int rr = row0 + r0 + i, t = rr / a.group, gq = rr - t * a.group;
-        T* out = (T*)a.out + d.x * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + lane * E;
-#pragma unroll
-        for (int e = 0; e < E; e += 2) *reinterpret_cast<typename Pack2<T>::type*>(out + e) = Pack2<T>::down(o[i][e] * inv, o[i][e + 1] * inv);
-        if (lane == 0 && a.lse) a.lse[((int64_t)d.x * a.T + t) * a.nq + head * a.group + gq] = (m[i] + log2f(l[i])) * 0.69314718055994531f;
-    }
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<typename Pack2<T>::type*>(out + e) = Pack2<T>::down(o[e] * inv, o[e + 1] * inv);
+    if (lane == 0 && a.lse) a.lse[((int64_t)d.x * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(l)) * 0.69314718055994531f;
 }
 
 }  // namespace jot

@@ -5,12 +5,14 @@
 //   pages: the head dimension runs along 128-byte rows (16-byte chunk c of row r at c ^ (r mod 8)), which is the first product's
 //   K-major operand for Q and K, and for V the second product's MN-major one, so nothing is transposed.
 //
-// Two streams of work share the tensor pipe, each with a score buffer, an accumulator, a warpgroup (thread = row) and a warp that
-// issues its products: while one stream's rows are in exponentials, the other's products run.  ROWS = 256: the streams are two tiles
-// of 128 rows over the same keys.  ROWS <= 128: they are the even and the odd tiles of keys over the same rows, and meet at the end.
-// With at most 64 or 32 rows the tile of 128 holds them twice or four times over, and each copy's threads take their share of a tile's keys
-// (the probabilities of the others are zeros): what a thread has to do for a tile, which is what few rows wait for, is a half or
-// a quarter, and the copies meet at the end as the streams do.
+// Two streams share the tensor pipe, each with a score buffer, an accumulator, a warpgroup (thread = row) and a warp that issues its
+// products: while one stream's rows are in exponentials, or on their way out, the other's products run.
+//   ROWS <= 128   each stream has a share of the line to itself, with queries and a stage of keys and values of its own, as if it were a CTA.
+//                 With at most 64 or 32 rows the tile of 128 holds them twice or four times over, and each copy's threads take their
+//                 share of a tile's keys (the probabilities of the others are zeros): what a thread has to do for a tile, which is what
+//                 few rows wait for, is a half or a quarter.  The copies are added up at the end.
+//   ROWS = 256    the streams are two tiles of 128 rows over the same keys, and take turns in their exponentials: at the same time, they
+//                 would only get half of the special function units each, and then both wait for the tensor pipe.
 // The reference maximum of a row follows a tile's maximum only when that exceeds it by more than 2^8 (probabilities up to 256
 // are as exact as those up to 1); then the row of the accumulator is rescaled in tensor memory.
 //
@@ -19,8 +21,11 @@
 // such requests.
 //
 //   warps 0-3, 4-7   softmax of stream 0 and 1
-//   by TMA           warp 8 keys and values, warps 9, 10 products, warp 11 queries
-//   by cp.async      warps 8-11 keys, values and queries (page entries two tiles ahead, row addresses one), warps 12, 13 products
+//   by TMA           warps 8, 9 keys, values and queries of a stream each (ROWS = 256: keys and values, queries); warps 10, 11 products
+//   by cp.async      warps 8-11 keys, values and queries (ROWS <= 128: two a stream), warps 12, 13 products
+//
+// Every barrier is waited on phase by phase by whoever waits on it, so that a parity says which phase is meant.  All waits end: one
+// that gives up makes the CTA leave, after its copies and products under way have ended.
 #pragma once
 #include "paged_attention.cuh"
 
@@ -32,16 +37,15 @@ constexpr int kUmmaPagedMaxCtas = 160;     // one per SM
 template <int HD>
 struct UmmaPagedSmem {
     static constexpr int TILE_BYTES = 128 * HD * 2;               // 128 rows: a tile of Q, K or V
-    // Of K and of V.  With ROWS <= 128 each stream has half of them to itself: nobody waits on a barrier whose phases it does not see one by
-    // one, so a parity says which phase is meant.
-    static constexpr int STAGES = HD == 128 ? 2 : 4;
-    static constexpr int DYN_BYTES = (2 + 2 * STAGES) * TILE_BYTES + 1024;      // two tiles of queries: the streams', or this part's and the next one's
+    static constexpr int STAGES = HD == 128 ? 2 : 4;              // of K and of V
+    static constexpr int DYN_BYTES = (2 + 2 * STAGES) * TILE_BYTES + 1024;      // and the streams' tiles of queries
 };
 
-template <bool TMA>
+template <int ROWS, bool TMA>
 struct UmmaPagedRoles {
-    static constexpr int PROD = 8, MMA = TMA ? 9 : 12, QUERY = TMA ? 11 : 8, QUERY_WARPS = TMA ? 1 : 4;
-    static constexpr int THREADS = TMA ? 384 : 448;
+    static constexpr bool TWO = ROWS == 256;
+    static constexpr int PROD = 8, PROD_WARPS = TMA ? 1 : (TWO ? 4 : 2);       // of a stream (TWO: of both)
+    static constexpr int MMA = TMA ? 10 : 12, THREADS = TMA ? 384 : 448;
 };
 // Keys of a tile that TMA brings, and whether it can: whole pages in 128 rows, or parts of 128 of a page.
 __host__ __device__ constexpr bool paged_tma_pages(int page_size) { return page_size % 8 == 0 && (page_size <= 128 || page_size % 128 == 0); }
@@ -71,7 +75,7 @@ __host__ __device__ constexpr uint32_t umma_idesc16(int M, int N, bool b_mn_majo
     return (1u << 4) | (fmt << 7) | (fmt << 10) | (uint32_t(b_mn_major) << 16) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
 }
 
-// The parts of items a CTA's share consists of, in order.
+// The parts of items that a share consists of, in order.
 struct PagedWalk {
     int b, n, nt, item, kt, cnt;          // sequence, its keys and tiles, item, first tile and number of tiles of this part
     int left;                             // tiles of the share from this part on
@@ -99,13 +103,14 @@ struct PagedWalk {
 };
 
 template <typename T, int HD, int ROWS, bool TMA>
-__global__ void __launch_bounds__(UmmaPagedRoles<TMA>::THREADS, 1)
+__global__ void __launch_bounds__(UmmaPagedRoles<ROWS, TMA>::THREADS, 1)
 paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV) {
     using SM = UmmaPagedSmem<HD>;
-    using Role = UmmaPagedRoles<TMA>;
-    constexpr bool TWO = ROWS == 256;
+    using Role = UmmaPagedRoles<ROWS, TMA>;
+    constexpr bool TWO = Role::TWO;
     constexpr int KB = HD / 64, ST = SM::STAGES, RING = TWO ? ST : ST / 2, TILE = kUmmaPagedTile, THREADS = Role::THREADS;
-    constexpr int MT = ROWS, REP = TWO ? 1 : 128 / ROWS, KC = 128 / REP;     // copies of a row, and keys of a tile that one takes
+    constexpr int STREAMS = TWO ? 1 : 2;                          // shares of the line a CTA has
+    constexpr int REP = TWO ? 1 : 128 / ROWS, KC = 128 / REP;     // copies of a row, and keys of a tile that one takes
     constexpr uint32_t IDESC_S = umma_idesc16<T>(128, 128, false), IDESC_O = umma_idesc16<T>(128, HD, true);
     constexpr uint32_t O_COL = 256;              // scores of the streams at columns 0 and 128, accumulators at 256 and 384
     constexpr float kRaise = 8.f;
@@ -113,11 +118,12 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * SM::TILE_BYTES, sV = sK + ST * SM::TILE_BYTES;
+    uint8_t* const values_at = smem + (2 + ST) * SM::TILE_BYTES;
     __shared__ uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], o_empty[2],
-        drain[2], tail_bar, prod_bar, x_bar, g_bar[2];
-    __shared__ uint64_t row_at[2][TMA ? 1 : 2 * TILE];     // by cp.async: addresses of a tile's key rows, then of its value rows; odd: no such row
-    __shared__ uint64_t row_q[MT];
-    __shared__ float2 x_ml[2][2][128];           // ROWS <= 128: [parity of the part][stream][row] (maximum, sum)
+        drain[2], turn[2], tail_bar, prod_bar[2], g_bar[2];
+    __shared__ uint64_t row_at[TMA ? 1 : STREAMS][2][TMA ? 1 : 2 * TILE];      // by cp.async: addresses of a tile's key rows, then of its value rows; odd: no such row
+    __shared__ uint64_t row_q[2][128];           // addresses of the queries
+    __shared__ float2 x_ml[2][REP > 1 ? 128 : 1];            // [stream][row] (maximum, sum) of the copies
     __shared__ PagedRangeSmem range_smem;
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag, drain_flag;
@@ -126,25 +132,24 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     if (tid == 0) {
         abort_flag = drain_flag = 0;
         for (int i = 0; i < ST; ++i) {
-            mbar_init(&k_full[i], TMA ? 1 : 128);          // by cp.async: every producer thread's requests
-            mbar_init(&k_empty[i], TWO ? 2 : 1);          // every stream that uses the tile
-            mbar_init(&v_full[i], TMA ? 1 : 128);
+            mbar_init(&k_full[i], TMA ? 1 : Role::PROD_WARPS * 32);          // by cp.async: every producer thread's requests
+            mbar_init(&k_empty[i], TWO ? 2 : 1);                             // every stream that uses the tile
+            mbar_init(&v_full[i], TMA ? 1 : Role::PROD_WARPS * 32);
             mbar_init(&v_empty[i], TWO ? 2 : 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&q_full[i], Role::QUERY_WARPS * 32);
-            mbar_init(&q_empty[i], 10);          // both streams' products; the softmax warps, which use the room at the end of a part
+            mbar_init(&q_full[i], Role::PROD_WARPS * 32);
+            mbar_init(&q_empty[i], TWO ? 8 : 4);                             // the softmax warps, which use the room at the end of a part
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
             mbar_init(&pv_done[i], 1);
-            mbar_init(&o_empty[i], TWO ? 4 : 8);         // the warps that read the accumulator
+            mbar_init(&o_empty[i], 4);
             mbar_init(&drain[i], 1);
+            mbar_init(&turn[i], 4);
+            mbar_init(&prod_bar[i], Role::PROD_WARPS);
+            mbar_init(&g_bar[i], 4);
         }
-        mbar_init(&prod_bar, Role::QUERY_WARPS);
-        mbar_init(&x_bar, 8);
         mbar_init(&tail_bar, 2);
-        mbar_init(&g_bar[0], 4);
-        mbar_init(&g_bar[1], 4);
         fence_barrier_init();
         fence_proxy_async_smem();
         if (TMA) {
@@ -156,7 +161,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     if (TMA && KEYS < TILE) {                    // value rows that no box covers: their probabilities are zero, so they must be numbers
         for (int i = tid; i < ST * KB * (TILE - KEYS) * 8; i += THREADS) {
             const int c = i & 7, r = (i >> 3) % (TILE - KEYS), t = (i >> 3) / (TILE - KEYS);
-            *reinterpret_cast<uint4*>(smem + (sV - sQ) + t * 16384 + (KEYS + r) * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(values_at + t * 16384 + (KEYS + r) * 128 + c * 16) = make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async_smem();
     }
@@ -173,19 +178,75 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     grid_launch_dependents();
     grid_dependency_wait();
 
-    const int R = a.T * a.group, RT = (R + MT - 1) / MT, per_b = a.nkv * RT;
-    const PagedRange rg = paged_range<T, HD, THREADS>(a, KEYS, per_b, range_smem);
-    if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    const int R = a.T * a.group, RT = (R + ROWS - 1) / ROWS, per_b = a.nkv * RT;
+    // the stream of this warp (TWO: 0 for the producers, who serve both)
+    const int s = warp < 8 ? warp >> 2 : (warp >= Role::MMA ? warp - Role::MMA : (TWO ? 0 : (warp - Role::PROD) / Role::PROD_WARPS));
+    const PagedRange rg = paged_range<T, HD, THREADS, STREAMS>(a, KEYS, per_b, TWO ? 0 : s, range_smem);
+    const int share = blockIdx.x * STREAMS + (TWO ? 0 : s);
+    if (tid < STREAMS) a.desc[blockIdx.x * STREAMS + tid] = make_int4(0, 0, 0, 0);
+    __syncthreads();                             // (a descriptor is written again below)
     auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {
         const bool w = mbar_wait(bar, parity, abortp);
         return __all_sync(0xffffffffu, w);
     };
 
-    if (rg.end > rg.begin) {
-        if (TMA && warp == Role::PROD) {
-            // ================================ producer by TMA: lane = page of the tile ================================
+    if (rg.end <= rg.begin) {
+        // no share
+    } else if (warp >= Role::PROD && warp < Role::MMA) {
+        // ================================ producers ================================
+        constexpr int PW = Role::PROD_WARPS, CPR = HD / 8, RPP = 32 / CPR;     // warps of the stream; chunks of a row; rows per request of a warp
+        const int pw = TMA ? 0 : (warp - Role::PROD) % PW, pt = pw * 32 + lane;
+        const int lr = lane / CPR, lc = lane % CPR;
+        // rows of one item's queries -> a tile
+        auto queries = [&](const PagedWalk& w, int q) -> bool {                // q: which tile of 128 of the item
+            const int head = w.item / RT, row0 = (w.item - head * RT) * ROWS + q * 128;
+            for (int i = pt; i < min(ROWS, 128); i += PW * 32) {
+                const int r = row0 + i, t = r / a.group, gq = r - t * a.group;
+                uint64_t at = reinterpret_cast<uint64_t>(a.q) | 1u;
+                if (r < R) at = reinterpret_cast<uint64_t>((const T*)a.q + w.b * a.q_b + t * a.q_t + (int64_t)(head * a.group + gq) * a.q_h);
+                row_q[TWO ? q : s][i] = at;
+            }
+            return true;
+        };
+        auto copy_queries = [&](int tile) {
+            constexpr int SHARE = 128 / PW;                        // rows of this warp
+#pragma unroll 8
+            for (int i = 0; i < SHARE / RPP; ++i) {
+                const int r = pw * SHARE + i * RPP + lr;
+                const uint64_t at = row_q[tile][TWO ? r : r % ROWS];
+                cp_async16(sQ + tile * SM::TILE_BYTES + (lc / 8) * 16384 + r * 128 + (((lc % 8) ^ (r & 7)) << 4),
+                           reinterpret_cast<const uint8_t*>(at & ~1ull) + lc * 16, !(at & 1));
+            }
+        };
+        uint32_t prod_ph = 0;
+        auto prod_sync = [&]() -> bool {                           // of the stream's producers
+            __syncwarp();
+            if (PW == 1) return true;
+            if (lane == 0) mbar_arrive(&prod_bar[s]);
+            const bool w = wait_all(&prod_bar[s], prod_ph);
+            prod_ph ^= 1;
+            return w;
+        };
+        auto fetch_queries = [&](const PagedWalk& w, uint32_t part) -> bool {
+            queries(w, 0);
+            if (TWO) queries(w, 1);
+            if (!prod_sync()) return false;
+            if (!wait_all(&q_empty[s], (part & 1) ^ 1)) return false;
+            copy_queries(s);
+            if (TWO) copy_queries(1);
+            cp_async_arrive(&q_full[s]);
+            return prod_sync();                                    // the addresses are used up
+        };
+        PagedWalk w(rg, KEYS);
+        bool ok = true, more = true;
+        if (TMA && TWO && warp == Role::PROD + 1) {
+            for (uint32_t part = 0; ok && more; ++part) {
+                ok = fetch_queries(w, part);
+                if (ok) more = w.next(a, per_b, KEYS);
+            }
+        } else if (TMA) {
+            // lane = page of the tile
             const int ps = a.pages.page_size, boxes = ps <= 128 ? KEYS / ps : 1, box = min(ps, 128);
-            PagedWalk w(rg, KEYS);
             PagedWalk ahead = w;                                   // the tile whose page entry is requested next
             int ahead_j = 0;
             bool ahead_more = true;
@@ -201,9 +262,8 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 }
             };
             request_entry();
-            uint32_t keys_sent[2] = {0, 0}, values_sent[2] = {0, 0};           // tiles per ring: a stream's, or both streams'
-            bool ok = true, more = true;
-            while (ok && more) {
+            uint32_t keys_sent = 0, values_sent = 0;
+            for (uint32_t part = 0; ok && more; ++part) {
                 const int head = w.item / RT;
                 for (int j = 0; j < w.cnt; ++j) {
                     const int first = (w.kt + j) * KEYS, key = first + lane * box;
@@ -225,71 +285,53 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                         }
                         __syncwarp();
                     };
-                    const int ring = TWO ? 0 : j & 1;
-                    const uint32_t at = keys_sent[ring], st = ring * RING + at % RING, ph = (at / RING & 1) ^ 1;
+                    const uint32_t st = (TWO ? 0 : s * RING) + keys_sent % RING, ph = (keys_sent / RING & 1) ^ 1;
                     if (!(ok = wait_all(&k_empty[st], ph))) break;
                     fetch(sK + st * SM::TILE_BYTES, &tmK, &k_full[st]);
-                    ++keys_sent[ring];
+                    ++keys_sent;
                     if (!(ok = wait_all(&v_empty[st], ph))) break;
                     fetch(sV + st * SM::TILE_BYTES, &tmV, &v_full[st]);
-                    ++values_sent[ring];
+                    ++values_sent;
+                    // (the queries' room is free later than the first tile's)
+                    if (!TWO && j == 0 && !(ok = fetch_queries(w, part))) break;
                 }
                 if (ok) more = w.next(a, per_b, KEYS);
             }
             // somebody gave up: what is on its way must land before this CTA's shared memory is another's
 #pragma unroll
-            for (int i = 0; !ok && i < ST; ++i) {
-                const uint32_t nk = (keys_sent[i / RING] + RING - 1 - i % RING) / RING, nv = (values_sent[i / RING] + RING - 1 - i % RING) / RING;
-                if (nk > 0) mbar_wait(&k_full[i], (nk - 1) & 1, &drain_flag);
-                if (nv > 0) mbar_wait(&v_full[i], (nv - 1) & 1, &drain_flag);
+            for (int i = 0; !ok && i < RING; ++i) {
+                const int st = (TWO ? 0 : s * RING) + i;
+                const uint32_t nk = (keys_sent + RING - 1 - i) / RING, nv = (values_sent + RING - 1 - i) / RING;
+                if (nk > 0) mbar_wait(&k_full[st], (nk - 1) & 1, &drain_flag);
+                if (nv > 0) mbar_wait(&v_full[st], (nv - 1) & 1, &drain_flag);
             }
-        } else if (warp >= Role::QUERY && warp < Role::QUERY + Role::QUERY_WARPS) {
-            // ================================ queries, and keys by cp.async ================================
-            const int pt = tid - Role::QUERY * 32, pw = pt >> 5;
-            constexpr int CPR = HD / 8, RPP = 32 / CPR;            // chunks of a row; rows per request of a warp
-            const int lr = lane / CPR, lc = lane % CPR;
-            uint32_t ldst[8 / RPP];                                // where this lane's chunk of a key goes: repeats every 8 rows
-#pragma unroll
-            for (int i = 0; i < 8 / RPP; ++i)
-                ldst[i] = (uint32_t)((lc / 8) * 16384 + (pw * 32 + i * RPP + lr) * 128 + (((lc % 8) ^ ((i * RPP + lr) & 7)) << 4));
+        } else {
+            constexpr int SHARE = 128 / PW;                        // rows of this warp
             auto copy_rows = [&](uint32_t dst, const uint64_t* rows) {
-#pragma unroll
-                for (int i = 0; i < 32 / RPP; ++i) {
-                    const uint64_t at = rows[pw * 32 + i * RPP + lr];
-                    cp_async16(dst + ldst[i % (8 / RPP)] + (i * RPP / 8) * 1024, reinterpret_cast<const uint8_t*>(at & ~1ull) + lc * 16, !(at & 1));
-                }
-            };
-            auto copy_queries = [&](uint32_t dst, const uint64_t* rows) {
-                constexpr int SHARE = 128 / Role::QUERY_WARPS;     // rows of this warp
 #pragma unroll 8
                 for (int i = 0; i < SHARE / RPP; ++i) {
                     const int r = pw * SHARE + i * RPP + lr;
-                    const uint64_t at = rows[TWO ? r : r % ROWS];
+                    const uint64_t at = rows[r];
                     cp_async16(dst + (lc / 8) * 16384 + r * 128 + (((lc % 8) ^ (r & 7)) << 4), reinterpret_cast<const uint8_t*>(at & ~1ull) + lc * 16, !(at & 1));
                 }
             };
-            uint32_t prod_ph = 0;
-            auto prod_sync = [&]() -> bool {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&prod_bar);
-                const bool w = wait_all(&prod_bar, prod_ph);
-                prod_ph ^= 1;
-                return w;
-            };
             // page entries two tiles ahead, addresses one
+            constexpr int MINE = 128 / (PW * 32);                  // keys of a tile a thread looks up
             int lb = rg.b, ln = rg.n, lkt = rg.kt, litem = rg.item, lleft = rg.end - rg.begin;
-            int page = 0, in_page = 0;
-            bool exists = false;
+            int page[MINE], in_page[MINE];
+            bool exists[MINE];
             auto request_entry = [&]() {
-                exists = false;
-                if (lleft <= 0) return;
-                const int key = lkt * TILE + pt;
-                if (key < ln) {
-                    const int p = key / a.pages.page_size;
-                    in_page = (litem / RT) * a.pages.page_size + key - p * a.pages.page_size;
-                    page = a.table[lb * a.table_stride + p];
-                    exists = true;
+#pragma unroll
+                for (int i = 0; i < MINE; ++i) {
+                    const int key = lkt * TILE + pt + i * PW * 32;
+                    exists[i] = lleft > 0 && key < ln;
+                    if (exists[i]) {
+                        const int p = key / a.pages.page_size;
+                        in_page[i] = (litem / RT) * a.pages.page_size + key - p * a.pages.page_size;
+                        page[i] = a.table[lb * a.table_stride + p];
+                    }
                 }
+                if (lleft <= 0) return;
                 --lleft;
                 if ((lkt + 1) * TILE < ln) {
                     ++lkt;
@@ -301,394 +343,344 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     }
                 }
             };
+            uint64_t(*const at)[2 * TILE] = reinterpret_cast<uint64_t(*)[2 * TILE]>(row_at[TMA || TWO ? 0 : s]);
             auto leave_address = [&](int buf) {
-                uint64_t ka = reinterpret_cast<uint64_t>(a.pages.k) | 1u, va = reinterpret_cast<uint64_t>(a.pages.v) | 1u;
-                if (exists) {
-                    if ((unsigned)page < (unsigned)a.pages.n_pages) {
-                        ka = reinterpret_cast<uint64_t>((const T*)a.pages.k + page * a.pages.k_page + (int64_t)in_page * HD);
-                        va = reinterpret_cast<uint64_t>((const T*)a.pages.v + page * a.pages.v_page + (int64_t)in_page * HD);
-                    } else if (a.status) {
-                        atomicExch(a.status, kStatusBadIndex);
-                    }
-                }
-                row_at[buf][pt] = ka;
-                row_at[buf][TILE + pt] = va;
-            };
-            PagedWalk w(rg, KEYS);
-            if (!TMA) {
-                request_entry();
-                leave_address(0);
-                request_entry();
-            }
-            uint32_t g = 0, part = 0, sent[2] = {0, 0};            // tiles and parts so far, tiles per ring
-            bool ok = true, more = true;
-            for (; ok && more; ++part) {
-                // queries of the part
-                const int head = w.item / RT, row0 = (w.item - head * RT) * MT;
-                const int qb = TWO ? 0 : (part & 1);
-                const uint32_t qph = TWO ? (part & 1) ^ 1 : ((part >> 1) & 1) ^ 1;
-                for (int i = pt; i < MT; i += Role::QUERY_WARPS * 32) {
-                    const int r = row0 + i, t = r / a.group, gq = r - t * a.group;
-                    uint64_t at = reinterpret_cast<uint64_t>(a.q) | 1u;
-                    if (r < R) at = reinterpret_cast<uint64_t>((const T*)a.q + w.b * a.q_b + t * a.q_t + (int64_t)(head * a.group + gq) * a.q_h);
-                    row_q[i] = at;
-                }
-                ok = prod_sync();
-                if (ok) ok = wait_all(&q_empty[qb], qph);
-                if (!ok) break;
 #pragma unroll
-                for (int i = 0; i < (TWO ? 2 : 1); ++i) copy_queries(sQ + (TWO ? i : qb) * SM::TILE_BYTES, row_q + i * 128);
-                cp_async_arrive(&q_full[qb]);
-                if (TMA && !(ok = prod_sync())) break;             // the addresses are used up
-                for (int j = 0; !TMA && j < w.cnt; ++j, ++g) {
-                    const int buf = g & 1, ring = TWO ? 0 : j & 1;
-                    const uint32_t st = ring * RING + sent[ring] % RING, ph = (sent[ring] / RING & 1) ^ 1;
-                    ++sent[ring];
+                for (int i = 0; i < MINE; ++i) {
+                    uint64_t ka = reinterpret_cast<uint64_t>(a.pages.k) | 1u, va = reinterpret_cast<uint64_t>(a.pages.v) | 1u;
+                    if (exists[i]) {
+                        if ((unsigned)page[i] < (unsigned)a.pages.n_pages) {
+                            ka = reinterpret_cast<uint64_t>((const T*)a.pages.k + page[i] * a.pages.k_page + (int64_t)in_page[i] * HD);
+                            va = reinterpret_cast<uint64_t>((const T*)a.pages.v + page[i] * a.pages.v_page + (int64_t)in_page[i] * HD);
+                        } else if (a.status) {
+                            atomicExch(a.status, kStatusBadIndex);
+                        }
+                    }
+                    at[buf][pt + i * PW * 32] = ka;
+                    at[buf][TILE + pt + i * PW * 32] = va;
+                }
+            };
+            request_entry();
+            leave_address(0);
+            request_entry();
+            uint32_t g = 0;                                        // tiles so far
+            for (uint32_t part = 0; ok && more; ++part) {
+                for (int j = 0; j < w.cnt; ++j, ++g) {
+                    const uint32_t st = (TWO ? 0 : s * RING) + g % RING, ph = (g / RING & 1) ^ 1;
                     ok = prod_sync();                              // the tile's addresses are there, the ones before are used up
                     if (ok) ok = wait_all(&k_empty[st], ph);
                     if (!ok) break;
-                    copy_rows(sK + st * SM::TILE_BYTES, row_at[buf]);
+                    copy_rows(sK + st * SM::TILE_BYTES, at[g & 1]);
                     cp_async_arrive(&k_full[st]);
-                    leave_address(buf ^ 1);
+                    leave_address((g & 1) ^ 1);
                     request_entry();
                     if (!(ok = wait_all(&v_empty[st], ph))) break;
-                    copy_rows(sV + st * SM::TILE_BYTES, row_at[buf] + TILE);
+                    copy_rows(sV + st * SM::TILE_BYTES, at[g & 1] + TILE);
                     cp_async_arrive(&v_full[st]);
+                    if (j == 0 && !(ok = fetch_queries(w, part))) break;
                 }
                 if (ok) more = w.next(a, per_b, KEYS);
             }
-        } else if (warp == Role::MMA || warp == Role::MMA + 1) {
-            // ================================ products of stream s ================================
-            const int s = warp - Role::MMA;
-            const bool elected = elect_one();
-            const uint64_t qd0 = umma_desc_k128(sQ) + (uint64_t)(TWO ? s * (SM::TILE_BYTES >> 4) : 0), kd0 = umma_desc_k128(sK), vd0 = umma_desc_mn128(sV);
-            const uint32_t d_s = tmem_base + s * 128, d_o = tmem_base + O_COL + s * 128;
-            PagedWalk w(rg, KEYS);
-            uint32_t part = 0, used = 0, made = 0, done = 0, tails = 0;        // parts, those with a tile of this stream, first and second products, tails so far
-            bool ok = true, more = true;
-            for (; ok && more; ++part) {
-                const int units = TWO ? w.cnt : (w.cnt + 1 - s) / 2;                  // tiles of this stream
-                const int qb = TWO ? 0 : (part & 1);
-                const int tail = w.n - (w.nt - 1) * KEYS;          // keys of the last tile of the sequence
-                const bool has_tail = TMA && w.kt + w.cnt == w.nt && tail < KEYS;
-                ok = wait_all(&q_full[qb], TWO ? (part & 1) : ((part >> 1) & 1));
-                if (ok) fence_proxy_async_smem();                  // the queries are written as threads write; the tensor pipe reads as copies do
-                auto issue_S = [&](int u) -> bool {
-                    const uint32_t st = (TWO ? 0 : s * RING) + made % RING;
-                    if (!wait_all(&k_full[st], made / RING & 1)) return false;
-                    // the score buffer holds the probabilities of the stream's previous tile until its second product is done
-                    if (done > 0 && !wait_all(&pv_done[s], (done - 1) & 1)) return false;
-                    if (!TMA) fence_proxy_async_smem();
-                    tc_fence_after();
-                    if (elected) {
-                        const uint64_t qd = qd0 + (uint64_t)(TWO ? 0 : qb * (SM::TILE_BYTES >> 4)), kd = kd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
+        }
+    } else if (warp >= Role::MMA) {
+        // ================================ products of stream s ================================
+        const bool elected = elect_one();
+        const uint64_t qd = umma_desc_k128(sQ + s * SM::TILE_BYTES), kd0 = umma_desc_k128(sK), vd0 = umma_desc_mn128(sV);
+        const uint32_t d_s = tmem_base + s * 128, d_o = tmem_base + O_COL + s * 128;
+        PagedWalk w(rg, KEYS);
+        uint32_t part = 0, made = 0, done = 0, tails = 0;          // parts, first and second products, tails so far
+        bool ok = true, more = true;
+        for (; ok && more; ++part) {
+            const int tail = w.n - (w.nt - 1) * KEYS;              // keys of the last tile of the sequence
+            const bool has_tail = TMA && w.kt + w.cnt == w.nt && tail < KEYS;
+            ok = wait_all(&q_full[TWO ? 0 : s], part & 1);
+            if (ok) fence_proxy_async_smem();                      // the queries are written as threads write; the tensor pipe reads as copies do
+            auto issue_S = [&]() -> bool {
+                const uint32_t st = (TWO ? 0 : s * RING) + made % RING;
+                if (!wait_all(&k_full[st], made / RING & 1)) return false;
+                // the score buffer holds the probabilities of the stream's previous tile until its second product is done
+                if (done > 0 && !wait_all(&pv_done[s], (done - 1) & 1)) return false;
+                if (!TMA) fence_proxy_async_smem();
+                tc_fence_after();
+                if (elected) {
+                    const uint64_t kd = kd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
 #pragma unroll
-                        for (int kb = 0; kb < KB; ++kb)
+                    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) umma_bf16(d_s, qd + kb * 1024 + 2 * k, kd + kb * 1024 + 2 * k, IDESC_S, (kb | k) != 0);
-                        umma_commit(&s_full[s]);
-                        umma_commit(&k_empty[st]);
-                        if (u == units - 1) umma_commit(&q_empty[qb]);
-                    }
-                    __syncwarp();
-                    ++made;
-                    return true;
-                };
-                auto issue_PV = [&](int u) -> bool {
-                    const int tile = TWO ? u : 2 * u + s;
-                    const uint32_t st = (TWO ? 0 : s * RING) + done % RING;
-                    if (!wait_all(&v_full[st], done / RING & 1)) return false;
-                    if (has_tail && tile == w.cnt - 1) {
-                        // value rows behind the sequence's end, whatever the page holds there, and those of boxes that were not fetched
-                        if (!TWO || s == 0) {
-                            for (int i = lane; i < KB * (KEYS - tail) * 8; i += 32) {
-                                const int r = tail + (i >> 3) % (KEYS - tail), kb = (i >> 3) / (KEYS - tail);
-                                *reinterpret_cast<uint4*>(smem + (sV - sQ) + st * SM::TILE_BYTES + kb * 16384 + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
-                            }
-                            fence_proxy_async_smem();
-                            __syncwarp();
-                        }
-                        if (TWO) {                                 // the streams' warps meet: both see the zeros, and neither is a tail ahead
-                            if (lane == 0) mbar_arrive(&tail_bar);
-                            if (!wait_all(&tail_bar, tails & 1)) return false;
-                        }
-                    }
-                    if (!wait_all(&p_full[s], done & 1)) return false;
-                    if (!TMA) fence_proxy_async_smem();
-                    tc_fence_after();
-                    if (elected) {
-                        const uint64_t vd = vd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) umma_bf16_ts(d_o, d_s + (k < 4 ? 8 * k : 64 + 8 * (k - 4)), vd + k * 128, IDESC_O, u > 0 || k > 0);
-                        umma_commit(&pv_done[s]);
-                        umma_commit(&v_empty[st]);
-                    }
-                    __syncwarp();
-                    ++done;
-                    return true;
-                };
-                if (ok && units > 0) ok = issue_S(0);
-                if (ok && units == 0 && lane == 0) mbar_arrive(&q_empty[qb]);
-                // the part's first products overwrite the accumulator: the previous part's rows must have left
-                if (ok && units > 0 && used++ > 0) ok = wait_all(&o_empty[s], (used - 2) & 1);
-                for (int u = 0; ok && u < units; ++u) {
-                    ok = issue_PV(u);
-                    if (ok && u + 1 < units) ok = issue_S(u + 1);
+                        for (int k = 0; k < 4; ++k) umma_bf16(d_s, qd + kb * 1024 + 2 * k, kd + kb * 1024 + 2 * k, IDESC_S, (kb | k) != 0);
+                    umma_commit(&s_full[s]);
+                    umma_commit(&k_empty[st]);
                 }
-                tails += has_tail;
-                if (ok) more = w.next(a, per_b, KEYS);
-            }
-            // the last arrivals the tensor pipe owes this CTA's barriers; where somebody gave up, the end of the products under way
-            if (ok) {
-                if (done > 0) wait_all(&v_empty[(TWO ? 0 : s * RING) + (done - 1) % RING], (done - 1) / RING & 1);
-            } else {
-                if (elected) umma_commit(&drain[s]);
                 __syncwarp();
-                mbar_wait(&drain[s], 0, &drain_flag);
+                ++made;
+                return true;
+            };
+            auto issue_PV = [&](int u) -> bool {
+                const uint32_t st = (TWO ? 0 : s * RING) + done % RING;
+                if (!wait_all(&v_full[st], done / RING & 1)) return false;
+                if (has_tail && u == w.cnt - 1) {
+                    // value rows behind the sequence's end, whatever the page holds there, and those of boxes that were not fetched
+                    if (!TWO || s == 0) {
+                        for (int i = lane; i < KB * (KEYS - tail) * 8; i += 32) {
+                            const int r = tail + (i >> 3) % (KEYS - tail), kb = (i >> 3) / (KEYS - tail);
+                            *reinterpret_cast<uint4*>(values_at + st * SM::TILE_BYTES + kb * 16384 + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    if (TWO) {                                     // the streams' warps meet: both see the zeros, and neither is a tail ahead
+                        if (lane == 0) mbar_arrive(&tail_bar);
+                        if (!wait_all(&tail_bar, tails & 1)) return false;
+                    }
+                }
+                if (!wait_all(&p_full[s], done & 1)) return false;
+                if (!TMA) fence_proxy_async_smem();
+                tc_fence_after();
+                if (elected) {
+                    const uint64_t vd = vd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) umma_bf16_ts(d_o, d_s + (k < 4 ? 8 * k : 64 + 8 * (k - 4)), vd + k * 128, IDESC_O, u > 0 || k > 0);
+                    umma_commit(&pv_done[s]);
+                    umma_commit(&v_empty[st]);
+                }
+                __syncwarp();
+                ++done;
+                return true;
+            };
+            if (ok) ok = issue_S();
+            // the part's first products overwrite the accumulator: the previous part's rows must have left
+            if (ok && part > 0) ok = wait_all(&o_empty[s], (part - 1) & 1);
+            for (int u = 0; ok && u < w.cnt; ++u) {
+                ok = issue_PV(u);
+                if (ok && u + 1 < w.cnt) ok = issue_S();
             }
+            tails += has_tail;
+            if (ok) more = w.next(a, per_b, KEYS);
+        }
+        // the last arrival the tensor pipe owes this CTA's barriers; where somebody gave up, the end of the products under way
+        if (ok) {
+            wait_all(&v_empty[(TWO ? 0 : s * RING) + (done - 1) % RING], (done - 1) / RING & 1);
         } else {
-            // ================================ softmax: thread = row of its stream ================================
-            const int s = warp >> 2, quad = warp & 3, r128 = quad * 32 + lane;
-            const int rep = TWO ? 0 : r128 / ROWS, wr = TWO ? s * 128 + quad * 32 : quad * 32 % ROWS;      // copy of the row; first row of the warp
-            const uint32_t lanes = tmem_base + (uint32_t(quad * 32) << 16), sc = lanes + s * 128;
-            const float c = a.scale_log2, none = c < 0.f ? INFINITY : -INFINITY;
-            PagedWalk w(rg, KEYS);
-            uint32_t done[2] = {0, 0}, part = 0, g_ph = 0;         // tiles of each stream so far
-            bool ok = true, more = true;
-            for (; ok && more; ++part) {
-                const int head = w.item / RT, row0 = (w.item - head * RT) * MT;
-                const bool idle = row0 + wr >= R;                  // none of the warp's rows exists: it only keeps the barriers going
-                const int mine = TWO ? w.cnt : (w.cnt + 1 - s) / 2, other = TWO ? w.cnt : (w.cnt + s) / 2;
-                float mc = -INFINITY, l = 0.f;
-                for (int i = 0; i < mine; ++i) {
-                    if (!(ok = wait_all(&s_full[s], (done[s] + i) & 1))) break;
-                    if (!idle) {
-                        tc_fence_after();
-                        // keys of the tile that exist, from the first one of this copy on
-                        const int limit = min(w.n - (w.kt + (TWO ? i : 2 * i + s)) * KEYS, KEYS) - rep * KC;
-                        float v[64], bm = none;
-                        auto maximum = [&](float* x, int first, int count) {
-                            if (limit < first + count) {
+            if (elected) umma_commit(&drain[s]);
+            __syncwarp();
+            mbar_wait(&drain[s], 0, &drain_flag);
+        }
+    } else {
+        // ================================ softmax: thread = row of its stream ================================
+        const int quad = warp & 3, r128 = quad * 32 + lane, base0 = TWO ? s * 128 : 0;             // row of the tile; first row of the tile in the item
+        const int rep = TWO ? 0 : r128 / ROWS, wr = base0 + (TWO ? quad * 32 : quad * 32 % ROWS);  // copy of the row; first row of the warp in the item
+        const uint32_t lanes = tmem_base + (uint32_t(quad * 32) << 16), sc = lanes + s * 128, acc = lanes + O_COL + s * 128;
+        const float c = a.scale_log2, none = c < 0.f ? INFINITY : -INFINITY;
+        float* const room = reinterpret_cast<float*>(smem + s * SM::TILE_BYTES);
+        PagedWalk w(rg, KEYS);
+        uint32_t done = 0, part = 0, g_ph = 0;                     // tiles, parts so far
+        bool ok = true, more = true;
+        auto group_sync = [&]() -> bool {                          // of the stream's four warps
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&g_bar[s]);
+            const bool r = wait_all(&g_bar[s], g_ph);
+            g_ph ^= 1;
+            return r;
+        };
+        for (; ok && more; ++part) {
+            const int head = w.item / RT, row0 = (w.item - head * RT) * ROWS;
+            const bool idle = row0 + wr >= R;                      // none of the warp's rows exists: it only keeps the barriers going
+            float mc = -INFINITY, l = 0.f;
+            for (int i = 0; i < w.cnt; ++i, ++done) {
+                if (!(ok = wait_all(&s_full[s], done & 1))) break;
+                if (TWO && !(ok = wait_all(&turn[s], (done & 1) ^ (s == 0)))) break;
+                if (!idle) {
+                    tc_fence_after();
+                    // keys of the tile that exist, from the first one of this copy on
+                    const int limit = min(w.n - (w.kt + i) * KEYS, KEYS) - rep * KC;
+                    float v[64], bm = none;
+                    auto maximum = [&](float* x, int first, int count) {
+                        if (limit < first + count) {
 #pragma unroll
-                                for (int t = 0; t < count; ++t)
-                                    if (first + t >= limit) x[t] = none;
-                            }
-                            if (c < 0.f) {
-#pragma unroll
-                                for (int t = 0; t < count; ++t) bm = fminf(bm, x[t]);
-                            } else {
-                                float b1 = none;
-#pragma unroll
-                                for (int t = 0; t < count; t += 4) {
-                                    bm = fmaxf(bm, fmaxf(x[t], x[t + 1]));
-                                    b1 = fmaxf(b1, fmaxf(x[t + 2], x[t + 3]));
-                                }
-                                bm = fmaxf(bm, b1);
-                            }
-                        };
-                        if (KC == 32) {
-                            tmem_ld32(sc + rep * 32, v);
-                            tmem_ld_wait_regs(v);
-                            maximum(v, 0, 32);
-                        } else {
-                            // with a whole row per thread: keys 0..63, then 64..127, which stay in registers
-#pragma unroll
-                            for (int half = 0; half < KC / 64; ++half) {
-                                tmem_ld32(sc + rep * KC + half * 64, v);
-                                tmem_ld32(sc + rep * KC + half * 64 + 32, v + 32);
-                                tmem_ld_wait_regs(v);
-                                tmem_ld_wait_regs(v + 32);
-                                maximum(v, half * 64, 64);
-                            }
+                            for (int t = 0; t < count; ++t)
+                                if (first + t >= limit) x[t] = none;
                         }
-                        const float bmc = bm * c;
-                        const bool raise = bmc > mc + kRaise || (mc == -INFINITY && bmc > -INFINITY);
-                        const bool shrink = raise && i > 0;
-                        const float f = shrink ? ex2_approx(mc - bmc) : 1.f;       // (a row without a finite score so far: its sum is zero)
-                        if (raise) mc = bmc;
-                        l *= f;
-                        const float base = mc == -INFINITY ? 0.f : mc;
-                        float l0 = 0.f, l1 = 0.f;
-                        // 32 scores -> 16 columns of probabilities: keys 0..63 of the tile in columns 0..31, 64..127 in columns 64..95
-                        auto probabilities = [&](const float* x, uint32_t col) {
-                            uint32_t packed[16];
+                        if (c < 0.f) {
 #pragma unroll
-                            for (int t = 0; t < 16; ++t) {
-                                const float e0 = ex2_approx(fmaf(x[2 * t], c, -base)), e1 = ex2_approx(fmaf(x[2 * t + 1], c, -base));
-                                l0 += e0;
-                                l1 += e1;
-                                typename Pack2<T>::type h2 = Pack2<T>::down(e0, e1);
-                                packed[t] = *reinterpret_cast<uint32_t*>(&h2);
-                            }
-                            tmem_st16(sc + col, packed);
-                        };
-                        if (KC < 128) {
-                            const uint32_t zeros[16] = {};
-#pragma unroll
-                            for (int q = 0; q < 4; ++q)            // the other copies' keys
-                                if (q / (KC / 32) != rep) tmem_st16(sc + (q >> 1) * 64 + (q & 1) * 16, zeros);
-                        }
-                        if (KC == 32) {
-                            probabilities(v, (rep >> 1) * 64 + (rep & 1) * 16);
-                        } else if (KC == 64) {
-                            probabilities(v, rep * 64);
-                            probabilities(v + 32, rep * 64 + 16);
+                            for (int t = 0; t < count; ++t) bm = fminf(bm, x[t]);
                         } else {
-                            // (columns 64..95 held scores that have just been read, columns 0..31 are written behind the reads of theirs)
-                            probabilities(v, 64);
-                            probabilities(v + 32, 80);
-                            tmem_ld32(sc, v);
-                            tmem_ld32(sc + 32, v + 32);
+                            float b1 = none;
+#pragma unroll
+                            for (int t = 0; t < count; t += 4) {
+                                bm = fmaxf(bm, fmaxf(x[t], x[t + 1]));
+                                b1 = fmaxf(b1, fmaxf(x[t + 2], x[t + 3]));
+                            }
+                            bm = fmaxf(bm, b1);
+                        }
+                    };
+                    if (KC == 32) {
+                        tmem_ld32(sc + rep * 32, v);
+                        tmem_ld_wait_regs(v);
+                        maximum(v, 0, 32);
+                    } else {
+                        // with a whole row per thread: keys 0..63, then 64..127, which stay in registers
+#pragma unroll
+                        for (int half = 0; half < KC / 64; ++half) {
+                            tmem_ld32(sc + rep * KC + half * 64, v);
+                            tmem_ld32(sc + rep * KC + half * 64 + 32, v + 32);
                             tmem_ld_wait_regs(v);
                             tmem_ld_wait_regs(v + 32);
-                            if (limit < 64) {
-#pragma unroll
-                                for (int t = 0; t < 64; ++t)
-                                    if (t >= limit) v[t] = none;
-                            }
-                            probabilities(v, 0);
-                            probabilities(v + 32, 16);
-                        }
-                        l += l0 + l1;
-                        if (__any_sync(0xffffffffu, shrink)) {
-                            // (the previous second product of this stream was done before these scores were made)
-#pragma unroll
-                            for (int ch = 0; ch < HD / 32; ++ch) {
-                                float o[32];
-                                tmem_ld32(lanes + O_COL + s * 128 + ch * 32, o);
-                                tmem_ld_wait_regs(o);
-#pragma unroll
-                                for (int t = 0; t < 32; ++t) o[t] *= f;
-                                tmem_st32(lanes + O_COL + s * 128 + ch * 32, o);
-                            }
-                        }
-                        tmem_st_wait();
-                        tc_fence_before();
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_full[s]);
-                }
-                if (!ok) break;
-                done[s] += mine;
-                done[s ^ 1] += other;
-                // ---- the part goes out ----
-                const bool begins = w.kt == 0, whole = begins && w.cnt == w.nt;
-                const int64_t slot = (int64_t)blockIdx.x * 2 + (begins ? 1 : 0);
-                // Each thread weighs what its lane holds of a row, and the rows leave through the room of the part's queries, which are used up: whole
-                // rows of 16-byte chunks (chunk e of row r at e ^ (r mod 8)), and copies of a row are added up on the way.  With ROWS <= 128 the
-                // streams meet here, too: a warpgroup has half of the columns of both accumulators.
-                constexpr int COLS = TWO ? HD : HD / 2, ROUND = COLS / 2, CH4 = ROUND / 4, SWZ = CH4 < 8 ? CH4 - 1 : 7;
-                constexpr int OWN = TWO ? 128 : ROWS, ITEMS = OWN * CH4 / 128;         // rows of the warpgroup; chunks of a round a thread takes
-                const int col0 = TWO ? 0 : s * COLS, base0 = TWO ? s * 128 : 0;
-                const bool both = !TWO && w.cnt > 1;
-                float wa = 1.f, wb = 0.f, m = mc, sum = l;
-                if (TWO) {
-                    ok = wait_all(&pv_done[s], (done[s] - 1) & 1);
-                } else {
-                    x_ml[part & 1][s][r128] = make_float2(mc, l);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&x_bar);
-                    ok = wait_all(&x_bar, part & 1);
-                    if (ok) ok = wait_all(&pv_done[0], (done[0] - 1) & 1);
-                    if (ok && both) ok = wait_all(&pv_done[1], (done[1] - 1) & 1);
-                    // maximum and sum over everything that has keys of the row
-                    const int rt = r128 % ROWS;
-                    m = -INFINITY;
-                    sum = 0.f;
-#pragma unroll
-                    for (int q = 0; q < REP; ++q) {
-                        m = fmaxf(m, x_ml[part & 1][0][q * ROWS + rt].x);
-                        if (both) m = fmaxf(m, x_ml[part & 1][1][q * ROWS + rt].x);
-                    }
-                    const float mb = m == -INFINITY ? 0.f : m;                 // (no finite score at all: sums are 0 or NaN)
-#pragma unroll
-                    for (int q = 0; q < REP; ++q) {
-                        const float2 x0 = x_ml[part & 1][0][q * ROWS + rt], x1 = x_ml[part & 1][1][q * ROWS + rt];
-                        sum += x0.y * (m == -INFINITY ? 1.f : ex2_approx(x0.x - mb));
-                        if (both) sum += x1.y * (m == -INFINITY ? 1.f : ex2_approx(x1.x - mb));
-                    }
-                    wa = m == -INFINITY ? 1.f : ex2_approx(x_ml[part & 1][0][r128].x - mb);
-                    wb = m == -INFINITY ? 1.f : ex2_approx(x_ml[part & 1][1][r128].x - mb);
-                }
-                if (!ok) break;
-                if (whole) {
-                    const float inv = 1.f / sum;
-                    wa *= inv;
-                    wb *= inv;
-                }
-                float* const room = reinterpret_cast<float*>(smem + (TWO ? s * SM::TILE_BYTES : (part & 1) * SM::TILE_BYTES + s * (SM::TILE_BYTES / 2)));
-                if (!idle) tc_fence_after();
-#pragma unroll
-                for (int round = 0; round < 2; ++round) {
-                    if (!idle) {
-#pragma unroll
-                        for (int c0 = 0; c0 < ROUND; c0 += 16) {
-                            float o[16], o2[16];
-                            tmem_ld16(lanes + O_COL + (TWO ? s * 128 : 0) + col0 + round * ROUND + c0, o);
-                            if (both) tmem_ld16(lanes + O_COL + 128 + col0 + round * ROUND + c0, o2);
-                            tmem_ld16_wait(o);
-                            if (both) tmem_ld16_wait(o2);
-#pragma unroll
-                            for (int x = 0; x < 16; ++x) o[x] = both ? o[x] * wa + o2[x] * wb : o[x] * wa;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                reinterpret_cast<float4*>(room + r128 * ROUND)[(c0 / 4 + e) ^ (lane & SWZ)] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                            maximum(v, half * 64, 64);
                         }
                     }
-                    if (round == 1) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) {
-                            mbar_arrive(&o_empty[TWO ? s : 0]);
-                            if (both) mbar_arrive(&o_empty[1]);
-                        }
-                    }
-                    // the warpgroup's rows are in the room
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&g_bar[s]);
-                    if (!(ok = wait_all(&g_bar[s], g_ph))) break;
-                    g_ph ^= 1;
-#pragma unroll 2
-                    for (int k = 0; k < ITEMS; ++k) {
-                        const int i = k * 128 + (tid & 127), rt = i / CH4, e = i % CH4, r = row0 + base0 + rt;
-                        if (r >= R) break;
-                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float bmc = bm * c;
+                    const bool raise = bmc > mc + kRaise || (mc == -INFINITY && bmc > -INFINITY);
+                    const bool shrink = raise && i > 0;
+                    const float f = shrink ? ex2_approx(mc - bmc) : 1.f;       // (a row without a finite score so far: its sum is zero)
+                    if (raise) mc = bmc;
+                    l *= f;
+                    const float base = mc == -INFINITY ? 0.f : mc;
+                    float l0 = 0.f, l1 = 0.f;
+                    // 32 scores -> 16 columns of probabilities: keys 0..63 of the tile in columns 0..31, 64..127 in columns 64..95
+                    auto probabilities = [&](const float* x, uint32_t col) {
+                        uint32_t packed[16];
 #pragma unroll
-                        for (int q = 0; q < REP; ++q) {
-                            const float4 y = reinterpret_cast<const float4*>(room + (q * ROWS + rt) * ROUND)[e ^ (rt & SWZ)];
-                            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                        for (int t = 0; t < 16; ++t) {
+                            const float e0 = ex2_approx(fmaf(x[2 * t], c, -base)), e1 = ex2_approx(fmaf(x[2 * t + 1], c, -base));
+                            l0 += e0;
+                            l1 += e1;
+                            typename Pack2<T>::type h2 = Pack2<T>::down(e0, e1);
+                            packed[t] = *reinterpret_cast<uint32_t*>(&h2);
                         }
-                        const int col = col0 + round * ROUND + 4 * e;
-                        if (whole) {
-                            const int t = r / a.group, gq = r - t * a.group;
-                            typename Pack2<T>::type lo = Pack2<T>::down(x.x, x.y), hi = Pack2<T>::down(x.z, x.w);
-                            *reinterpret_cast<uint2*>((T*)a.out + w.b * a.o_b + t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + col) =
-                                make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
-                        } else {
-                            *reinterpret_cast<float4*>(a.partial + (slot * MT + base0 + rt) * HD + col) = x;
+                        tmem_st16(sc + col, packed);
+                    };
+                    if (KC < 128) {
+                        const uint32_t zeros[16] = {};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)                // the other copies' keys
+                            if (q / (KC / 32) != rep) tmem_st16(sc + (q >> 1) * 64 + (q & 1) * 16, zeros);
+                    }
+                    if (KC == 32) {
+                        probabilities(v, (rep >> 1) * 64 + (rep & 1) * 16);
+                    } else if (KC == 64) {
+                        probabilities(v, rep * 64);
+                        probabilities(v + 32, rep * 64 + 16);
+                    } else {
+                        // (columns 64..95 held scores that have just been read, columns 0..31 are written behind the reads of theirs)
+                        probabilities(v, 64);
+                        probabilities(v + 32, 80);
+                        tmem_ld32(sc, v);
+                        tmem_ld32(sc + 32, v + 32);
+                        tmem_ld_wait_regs(v);
+                        tmem_ld_wait_regs(v + 32);
+                        if (limit < 64) {
+#pragma unroll
+                            for (int t = 0; t < 64; ++t)
+                                if (t >= limit) v[t] = none;
+                        }
+                        probabilities(v, 0);
+                        probabilities(v + 32, 16);
+                    }
+                    l += l0 + l1;
+                    if (__any_sync(0xffffffffu, shrink)) {
+                        // (the previous second product of this stream was done before these scores were made)
+#pragma unroll
+                        for (int ch = 0; ch < HD / 32; ++ch) {
+                            float o[32];
+                            tmem_ld32(acc + ch * 32, o);
+                            tmem_ld_wait_regs(o);
+#pragma unroll
+                            for (int t = 0; t < 32; ++t) o[t] *= f;
+                            tmem_st32(acc + ch * 32, o);
                         }
                     }
-                    __syncwarp();
-                    if (round == 0) {
-                        if (lane == 0) mbar_arrive(&g_bar[s]);
-                        if (!(ok = wait_all(&g_bar[s], g_ph))) break;
-                        g_ph ^= 1;
-                    }
+                    tmem_st_wait();
+                    tc_fence_before();
                 }
-                if (!ok) break;
-                if (lane == 0) mbar_arrive(&q_empty[TWO ? 0 : part & 1]);
-                // (of the copies of a row, the first)
-                if (r128 < OWN && (TWO || s == 0) && row0 + base0 + r128 < R) {
-                    const int r = row0 + base0 + r128, t = r / a.group, gq = r - t * a.group;
-                    if (!whole) a.partial_ml[slot * MT + base0 + r128] = make_float2(m, sum);
-                    else if (a.lse) a.lse[((int64_t)w.b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(sum)) * 0.69314718055994531f;
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&p_full[s]);
+                    if (TWO) mbar_arrive(&turn[s ^ 1]);
                 }
-                if (begins && !whole && tid == 0) {
-                    const int last = rg.end + (w.nt - w.cnt) - 1;
-                    a.desc[blockIdx.x] = make_int4(w.b, w.item, paged_owner(rg.total, rg.ctas, last) - (int)blockIdx.x + 1, 0);
-                }
-                more = w.next(a, per_b, KEYS);
             }
+            if (!ok) break;
+            // ---- the part goes out ----
+            // Each thread weighs what its lane holds of a row, and the rows leave through the room of the part's queries, which are used up: whole
+            // rows of 16-byte chunks (chunk e of row r at e ^ (r mod 8)), the copies of a row added up on the way.
+            constexpr int ROUND = HD / 2, CH4 = ROUND / 4, OWN = TWO ? 128 : ROWS, ITEMS = OWN * CH4 / 128;    // columns of a round; chunks; rows; chunks a thread takes
+            const bool begins = w.kt == 0, whole = begins && w.cnt == w.nt;
+            const int64_t slot = (int64_t)share * 2 + (begins ? 1 : 0);
+            float weight = 1.f, m = mc, sum = l;
+            if (REP > 1) {
+                x_ml[s][r128] = make_float2(mc, l);
+                if (!(ok = group_sync())) break;
+                // maximum and sum over the copies
+                const int rt = r128 % ROWS;
+                m = -INFINITY;
+                sum = 0.f;
+#pragma unroll
+                for (int q = 0; q < REP; ++q) m = fmaxf(m, x_ml[s][q * ROWS + rt].x);
+                const float mb = m == -INFINITY ? 0.f : m;         // (no finite score at all: every copy's exponentials are against 0)
+#pragma unroll
+                for (int q = 0; q < REP; ++q) {
+                    const float2 x = x_ml[s][q * ROWS + rt];
+                    sum += x.y * (m == -INFINITY ? 1.f : ex2_approx(x.x - mb));
+                }
+                weight = m == -INFINITY ? 1.f : ex2_approx(mc - mb);
+            }
+            if (whole) weight *= 1.f / sum;
+            if (!(ok = wait_all(&pv_done[s], (done - 1) & 1))) break;
+            if (!idle) tc_fence_after();
+#pragma unroll
+            for (int round = 0; round < 2; ++round) {
+                if (!idle) {
+#pragma unroll
+                    for (int c0 = 0; c0 < ROUND; c0 += 32) {
+                        float o[32];
+                        tmem_ld32(acc + round * ROUND + c0, o);
+                        tmem_ld_wait_regs(o);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            reinterpret_cast<float4*>(room + r128 * ROUND)[(c0 / 4 + e) ^ (lane & 7)] =
+                                make_float4(o[4 * e] * weight, o[4 * e + 1] * weight, o[4 * e + 2] * weight, o[4 * e + 3] * weight);
+                    }
+                }
+                if (round == 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&o_empty[s]);
+                }
+                if (!(ok = group_sync())) break;                   // the stream's rows are in the room
+#pragma unroll 2
+                for (int k = 0; k < ITEMS; ++k) {
+                    const int i = k * 128 + (tid & 127), rt = i / CH4, e = i % CH4, r = row0 + base0 + rt;
+                    if (r >= R) break;
+                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int q = 0; q < REP; ++q) {
+                        const float4 y = reinterpret_cast<const float4*>(room + (q * ROWS + rt) * ROUND)[e ^ (rt & 7)];
+                        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                    }
+                    const int col = round * ROUND + 4 * e;
+                    if (whole) {
+                        const int t = r / a.group, gq = r - t * a.group;
+                        typename Pack2<T>::type lo = Pack2<T>::down(x.x, x.y), hi = Pack2<T>::down(x.z, x.w);
+                        *reinterpret_cast<uint2*>((T*)a.out + w.b * a.o_b + t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + col) =
+                            make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+                    } else {
+                        *reinterpret_cast<float4*>(a.partial + (slot * ROWS + base0 + rt) * HD + col) = x;
+                    }
+                }
+                if (round == 0 && !(ok = group_sync())) break;     // the room is read
+            }
+            if (!ok) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_empty[TWO ? 0 : s]);
+            if (r128 < OWN && row0 + base0 + r128 < R) {           // (of the copies of a row, the first)
+                const int r = row0 + base0 + r128, t = r / a.group, gq = r - t * a.group;
+                if (!whole) a.partial_ml[slot * ROWS + base0 + r128] = make_float2(m, sum);
+                else if (a.lse) a.lse[((int64_t)w.b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(sum)) * 0.69314718055994531f;
+            }
+            if (begins && !whole && (tid & 127) == 0 && (!TWO || s == 0)) {
+                const int last = rg.end + (w.nt - w.cnt) - 1;      // the item's last tile on the line: the next shares have the rest of it
+                a.desc[share] = make_int4(w.b, w.item, paged_owner(rg.total, rg.ctas, last) - share + 1, 0);
+            }
+            more = w.next(a, per_b, KEYS);
         }
     }
     cp_async_wait<0>();
