@@ -134,18 +134,18 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
     PagedRange rg;
     int in_seq = 0;
     const int first = tiles_of(a.B <= 32 ? lane : tid);
-    auto cut = [&](int stream, int& begin, int& end) {
-        const int i = blockIdx.x * STREAMS + stream;
-        begin = i < rg.ctas ? paged_share(rg.total, rg.ctas, i) : 0;
-        end = i < rg.ctas ? paged_share(rg.total, rg.ctas, i + 1) : 0;
+    auto cut = [](int total, int stream, int& begin, int& end) {
+        const int ctas = min((int)gridDim.x * STREAMS, total), i = blockIdx.x * STREAMS + stream;
+        begin = i < ctas ? paged_share(total, ctas, i) : 0;
+        end = i < ctas ? paged_share(total, ctas, i + 1) : 0;
+        return ctas;
     };
     rg.b = 0;
     if (a.B <= 32) {                // every warp for itself
         const int inc = scan(first);
         rg.total = __shfl_sync(0xffffffffu, inc, 31);
-        rg.ctas = min((int)gridDim.x * STREAMS, rg.total);
         empty = __any_sync(0xffffffffu, empty);
-        cut(mine, rg.begin, rg.end);
+        rg.ctas = cut(rg.total, mine, rg.begin, rg.end);
         if (rg.end > rg.begin) {
             rg.b = __popc(__ballot_sync(0xffffffffu, inc <= rg.begin));        // sequences that end before it
             in_seq = rg.begin - __shfl_sync(0xffffffffu, inc - first, rg.b);
@@ -162,8 +162,7 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
             return t;
         };
         rg.total = totals(WARPS);
-        rg.ctas = min((int)gridDim.x * STREAMS, rg.total);
-        cut(mine, rg.begin, rg.end);
+        rg.ctas = cut(rg.total, mine, rg.begin, rg.end);
         int before = 0;
         for (int b0 = 0; b0 < a.B; b0 += THREADS) {
             const int tiles = b0 == 0 ? first : tiles_of(b0 + tid), inc = scan(tiles);
@@ -174,7 +173,7 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
 #pragma unroll
             for (int i = 0; i < STREAMS; ++i) {
                 int begin, end;
-                cut(i, begin, end);
+                cut(rg.total, i, begin, end);
                 if (start <= begin && begin < start + tiles && begin < end) {
                     sm.b[i] = b0 + tid;
                     sm.in_seq[i] = begin - start;

@@ -21,8 +21,9 @@
 // such requests.
 //
 //   warps 0-3, 4-7   softmax of stream 0 and 1
-//   by TMA           warps 8, 9 keys, values and queries of a stream each (ROWS = 256: keys and values, queries); warps 10, 11 products
-//   by cp.async      warps 8-11 keys, values and queries (ROWS <= 128: two a stream), warps 12, 13 products
+//   by TMA           warps 8, 9 keys and values of a stream each (ROWS = 256: warp 8 of both), warps 10, 11 products
+//   by cp.async      warps 8-11 keys and values (ROWS <= 128: two a stream), warps 12, 13 products
+// The softmax warps bring the queries themselves, when a part begins: their room is the one that the previous part has left through.
 //
 // Every barrier is waited on phase by phase by whoever waits on it, so that a parity says which phase is meant.  All waits end: one
 // that gives up makes the CTA leave, after its copies and products under way have ended.
@@ -119,10 +120,10 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * SM::TILE_BYTES, sV = sK + ST * SM::TILE_BYTES;
     uint8_t* const values_at = smem + (2 + ST) * SM::TILE_BYTES;
-    __shared__ uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], o_empty[2],
+    __shared__ uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], q_full[2], s_full[2], p_full[2], pv_done[2], o_empty[2],
         drain[2], turn[2], tail_bar, prod_bar[2], g_bar[2];
     __shared__ uint64_t row_at[TMA ? 1 : STREAMS][2][TMA ? 1 : 2 * TILE];      // by cp.async: addresses of a tile's key rows, then of its value rows; odd: no such row
-    __shared__ uint64_t row_q[2][128];           // addresses of the queries
+    __shared__ uint64_t row_q[2][128], row_o[2][2][128];     // addresses of the rows' queries, and of their results ([parity of the part])
     __shared__ float2 x_ml[2][REP > 1 ? 128 : 1];            // [stream][row] (maximum, sum) of the copies
     __shared__ PagedRangeSmem range_smem;
     __shared__ uint32_t tmem_base_slot;
@@ -138,8 +139,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
             mbar_init(&v_empty[i], TWO ? 2 : 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&q_full[i], Role::PROD_WARPS * 32);
-            mbar_init(&q_empty[i], TWO ? 8 : 4);                             // the softmax warps, which use the room at the end of a part
+            mbar_init(&q_full[i], 128);                                      // every softmax thread's requests
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
             mbar_init(&pv_done[i], 1);
@@ -159,10 +159,8 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     }
     const int KEYS = TMA ? paged_tma_keys(a.pages.page_size) : TILE;       // of a tile
     if (TMA && KEYS < TILE) {                    // value rows that no box covers: their probabilities are zero, so they must be numbers
-        for (int i = tid; i < ST * KB * (TILE - KEYS) * 8; i += THREADS) {
-            const int c = i & 7, r = (i >> 3) % (TILE - KEYS), t = (i >> 3) / (TILE - KEYS);
-            *reinterpret_cast<uint4*>(values_at + t * 16384 + (KEYS + r) * 128 + c * 16) = make_uint4(0, 0, 0, 0);
-        }
+        for (int t = 0; t < ST * KB; ++t)
+            for (int i = tid; i < (TILE - KEYS) * 8; i += THREADS) reinterpret_cast<uint4*>(values_at + t * 16384 + KEYS * 128)[i] = make_uint4(0, 0, 0, 0);
         fence_proxy_async_smem();
     }
     if (warp == Role::MMA) {
@@ -197,27 +195,6 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         constexpr int PW = Role::PROD_WARPS, CPR = HD / 8, RPP = 32 / CPR;     // warps of the stream; chunks of a row; rows per request of a warp
         const int pw = TMA ? 0 : (warp - Role::PROD) % PW, pt = pw * 32 + lane;
         const int lr = lane / CPR, lc = lane % CPR;
-        // rows of one item's queries -> a tile
-        auto queries = [&](const PagedWalk& w, int q) -> bool {                // q: which tile of 128 of the item
-            const int head = w.item / RT, row0 = (w.item - head * RT) * ROWS + q * 128;
-            for (int i = pt; i < min(ROWS, 128); i += PW * 32) {
-                const int r = row0 + i, t = r / a.group, gq = r - t * a.group;
-                uint64_t at = reinterpret_cast<uint64_t>(a.q) | 1u;
-                if (r < R) at = reinterpret_cast<uint64_t>((const T*)a.q + w.b * a.q_b + t * a.q_t + (int64_t)(head * a.group + gq) * a.q_h);
-                row_q[TWO ? q : s][i] = at;
-            }
-            return true;
-        };
-        auto copy_queries = [&](int tile) {
-            constexpr int SHARE = 128 / PW;                        // rows of this warp
-#pragma unroll 8
-            for (int i = 0; i < SHARE / RPP; ++i) {
-                const int r = pw * SHARE + i * RPP + lr;
-                const uint64_t at = row_q[tile][TWO ? r : r % ROWS];
-                cp_async16(sQ + tile * SM::TILE_BYTES + (lc / 8) * 16384 + r * 128 + (((lc % 8) ^ (r & 7)) << 4),
-                           reinterpret_cast<const uint8_t*>(at & ~1ull) + lc * 16, !(at & 1));
-            }
-        };
         uint32_t prod_ph = 0;
         auto prod_sync = [&]() -> bool {                           // of the stream's producers
             __syncwarp();
@@ -227,23 +204,10 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
             prod_ph ^= 1;
             return w;
         };
-        auto fetch_queries = [&](const PagedWalk& w, uint32_t part) -> bool {
-            queries(w, 0);
-            if (TWO) queries(w, 1);
-            if (!prod_sync()) return false;
-            if (!wait_all(&q_empty[s], (part & 1) ^ 1)) return false;
-            copy_queries(s);
-            if (TWO) copy_queries(1);
-            cp_async_arrive(&q_full[s]);
-            return prod_sync();                                    // the addresses are used up
-        };
         PagedWalk w(rg, KEYS);
         bool ok = true, more = true;
         if (TMA && TWO && warp == Role::PROD + 1) {
-            for (uint32_t part = 0; ok && more; ++part) {
-                ok = fetch_queries(w, part);
-                if (ok) more = w.next(a, per_b, KEYS);
-            }
+            // nothing to bring
         } else if (TMA) {
             // lane = page of the tile
             const int ps = a.pages.page_size, boxes = ps <= 128 ? KEYS / ps : 1, box = min(ps, 128);
@@ -263,7 +227,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
             };
             request_entry();
             uint32_t keys_sent = 0, values_sent = 0;
-            for (uint32_t part = 0; ok && more; ++part) {
+            while (ok && more) {
                 const int head = w.item / RT;
                 for (int j = 0; j < w.cnt; ++j) {
                     const int first = (w.kt + j) * KEYS, key = first + lane * box;
@@ -292,8 +256,6 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     if (!(ok = wait_all(&v_empty[st], ph))) break;
                     fetch(sV + st * SM::TILE_BYTES, &tmV, &v_full[st]);
                     ++values_sent;
-                    // (the queries' room is free later than the first tile's)
-                    if (!TWO && j == 0 && !(ok = fetch_queries(w, part))) break;
                 }
                 if (ok) more = w.next(a, per_b, KEYS);
             }
@@ -364,7 +326,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
             leave_address(0);
             request_entry();
             uint32_t g = 0;                                        // tiles so far
-            for (uint32_t part = 0; ok && more; ++part) {
+            while (ok && more) {
                 for (int j = 0; j < w.cnt; ++j, ++g) {
                     const uint32_t st = (TWO ? 0 : s * RING) + g % RING, ph = (g / RING & 1) ^ 1;
                     ok = prod_sync();                              // the tile's addresses are there, the ones before are used up
@@ -377,7 +339,6 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     if (!(ok = wait_all(&v_empty[st], ph))) break;
                     copy_rows(sV + st * SM::TILE_BYTES, at[g & 1] + TILE);
                     cp_async_arrive(&v_full[st]);
-                    if (j == 0 && !(ok = fetch_queries(w, part))) break;
                 }
                 if (ok) more = w.next(a, per_b, KEYS);
             }
@@ -393,7 +354,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         for (; ok && more; ++part) {
             const int tail = w.n - (w.nt - 1) * KEYS;              // keys of the last tile of the sequence
             const bool has_tail = TMA && w.kt + w.cnt == w.nt && tail < KEYS;
-            ok = wait_all(&q_full[TWO ? 0 : s], part & 1);
+            ok = wait_all(&q_full[s], part & 1);
             if (ok) fence_proxy_async_smem();                      // the queries are written as threads write; the tensor pipe reads as copies do
             auto issue_S = [&]() -> bool {
                 const uint32_t st = (TWO ? 0 : s * RING) + made % RING;
@@ -421,10 +382,9 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 if (has_tail && u == w.cnt - 1) {
                     // value rows behind the sequence's end, whatever the page holds there, and those of boxes that were not fetched
                     if (!TWO || s == 0) {
-                        for (int i = lane; i < KB * (KEYS - tail) * 8; i += 32) {
-                            const int r = tail + (i >> 3) % (KEYS - tail), kb = (i >> 3) / (KEYS - tail);
-                            *reinterpret_cast<uint4*>(values_at + st * SM::TILE_BYTES + kb * 16384 + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
-                        }
+                        for (int kb = 0; kb < KB; ++kb)
+                            for (int i = lane; i < (KEYS - tail) * 8; i += 32)
+                                reinterpret_cast<uint4*>(values_at + st * SM::TILE_BYTES + kb * 16384 + tail * 128)[i] = make_uint4(0, 0, 0, 0);
                         fence_proxy_async_smem();
                         __syncwarp();
                     }
@@ -485,10 +445,28 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         for (; ok && more; ++part) {
             const int head = w.item / RT, row0 = (w.item - head * RT) * ROWS;
             const bool idle = row0 + wr >= R;                      // none of the warp's rows exists: it only keeps the barriers going
+            {
+                // this thread's row (of the copies of a row, each), then the stream's rows together: whole rows a request
+                constexpr int CPR = HD / 8, RPP = 32 / CPR;
+                const int r = row0 + base0 + (TWO ? r128 : r128 % ROWS), t = r / a.group, gq = r - t * a.group;
+                uint64_t at = reinterpret_cast<uint64_t>(a.q) | 1u;        // odd: no such row, zeros are written
+                if (r < R) at = reinterpret_cast<uint64_t>((const T*)a.q + w.b * a.q_b + t * a.q_t + (int64_t)(head * a.group + gq) * a.q_h);
+                row_q[s][r128] = at;
+                row_o[part & 1][s][r128] = reinterpret_cast<uint64_t>((T*)a.out + w.b * a.o_b + t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h);
+                if (!(ok = group_sync())) break;                   // (which the room of the previous part is read by, too)
+                const int lr = lane / CPR, lc = lane % CPR;
+#pragma unroll
+                for (int i = 0; i < 32 / RPP; ++i) {
+                    const int rr = quad * 32 + i * RPP + lr;
+                    const uint64_t from = row_q[s][rr];
+                    cp_async16(sQ + s * SM::TILE_BYTES + (lc / 8) * 16384 + rr * 128 + (((lc % 8) ^ (rr & 7)) << 4),
+                               reinterpret_cast<const uint8_t*>(from & ~1ull) + lc * 16, !(from & 1));
+                }
+                cp_async_arrive(&q_full[s]);
+            }
             float mc = -INFINITY, l = 0.f;
             for (int i = 0; i < w.cnt; ++i, ++done) {
                 if (!(ok = wait_all(&s_full[s], done & 1))) break;
-                if (TWO && !(ok = wait_all(&turn[s], (done & 1) ^ (s == 0)))) break;
                 if (!idle) {
                     tc_fence_after();
                     // keys of the tile that exist, from the first one of this copy on
@@ -528,6 +506,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                             maximum(v, half * 64, 64);
                         }
                     }
+                    if (TWO && !(ok = wait_all(&turn[s], (done & 1) ^ (s == 0)))) break;       // the other stream is through with its exponentials
                     const float bmc = bm * c;
                     const bool raise = bmc > mc + kRaise || (mc == -INFINITY && bmc > -INFINITY);
                     const bool shrink = raise && i > 0;
@@ -577,6 +556,8 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                         probabilities(v + 32, 16);
                     }
                     l += l0 + l1;
+                    __syncwarp();
+                    if (TWO && lane == 0) mbar_arrive(&turn[s ^ 1]);
                     if (__any_sync(0xffffffffu, shrink)) {
                         // (the previous second product of this stream was done before these scores were made)
 #pragma unroll
@@ -591,12 +572,12 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     }
                     tmem_st_wait();
                     tc_fence_before();
+                } else if (TWO) {
+                    if (!(ok = wait_all(&turn[s], (done & 1) ^ (s == 0)))) break;
+                    if (lane == 0) mbar_arrive(&turn[s ^ 1]);
                 }
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&p_full[s]);
-                    if (TWO) mbar_arrive(&turn[s ^ 1]);
-                }
+                if (lane == 0) mbar_arrive(&p_full[s]);
             }
             if (!ok) break;
             // ---- the part goes out ----
@@ -658,9 +639,8 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     }
                     const int col = round * ROUND + 4 * e;
                     if (whole) {
-                        const int t = r / a.group, gq = r - t * a.group;
                         typename Pack2<T>::type lo = Pack2<T>::down(x.x, x.y), hi = Pack2<T>::down(x.z, x.w);
-                        *reinterpret_cast<uint2*>((T*)a.out + w.b * a.o_b + t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + col) =
+                        *reinterpret_cast<uint2*>(reinterpret_cast<T*>(row_o[part & 1][s][rt]) + col) =
                             make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
                     } else {
                         *reinterpret_cast<float4*>(a.partial + (slot * ROWS + base0 + rt) * HD + col) = x;
@@ -669,8 +649,6 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 if (round == 0 && !(ok = group_sync())) break;     // the room is read
             }
             if (!ok) break;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&q_empty[TWO ? 0 : s]);
             if (r128 < OWN && row0 + base0 + r128 < R) {           // (of the copies of a row, the first)
                 const int r = row0 + base0 + r128, t = r / a.group, gq = r - t * a.group;
                 if (!whole) a.partial_ml[slot * ROWS + base0 + r128] = make_float2(m, sum);
