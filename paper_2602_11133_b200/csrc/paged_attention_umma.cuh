@@ -471,7 +471,8 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     tc_fence_after();
                     // keys of the tile that exist, from the first one of this copy on
                     const int limit = min(w.n - (w.kt + i) * KEYS, KEYS) - rep * KC;
-                    float v[64], bm = none;
+                    constexpr bool WIDE = TMA && KC == 128;        // room for all of a row's scores in registers
+                    float v[64], v2[WIDE ? 64 : 1], bm = none;
                     auto maximum = [&](float* x, int first, int count) {
                         if (limit < first + count) {
 #pragma unroll
@@ -491,10 +492,21 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                             bm = fmaxf(bm, b1);
                         }
                     };
-                    if (KC == 32) {
+                    if constexpr (KC == 32) {
                         tmem_ld32(sc + rep * 32, v);
                         tmem_ld_wait_regs(v);
                         maximum(v, 0, 32);
+                    } else if constexpr (WIDE) {
+                        tmem_ld32(sc, v);
+                        tmem_ld32(sc + 32, v + 32);
+                        tmem_ld32(sc + 64, v2);
+                        tmem_ld32(sc + 96, v2 + 32);
+                        tmem_ld_wait_regs(v);
+                        tmem_ld_wait_regs(v + 32);
+                        tmem_ld_wait_regs(v2);
+                        tmem_ld_wait_regs(v2 + 32);
+                        maximum(v, 0, 64);
+                        maximum(v2, 64, 64);
                     } else {
                         // with a whole row per thread: keys 0..63, then 64..127, which stay in registers
 #pragma unroll
@@ -534,11 +546,16 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                         for (int q = 0; q < 4; ++q)                // the other copies' keys
                             if (q / (KC / 32) != rep) tmem_st16(sc + (q >> 1) * 64 + (q & 1) * 16, zeros);
                     }
-                    if (KC == 32) {
+                    if constexpr (KC == 32) {
                         probabilities(v, (rep >> 1) * 64 + (rep & 1) * 16);
-                    } else if (KC == 64) {
+                    } else if constexpr (KC == 64) {
                         probabilities(v, rep * 64);
                         probabilities(v + 32, rep * 64 + 16);
+                    } else if constexpr (WIDE) {
+                        probabilities(v, 0);
+                        probabilities(v + 32, 16);
+                        probabilities(v2, 64);
+                        probabilities(v2 + 32, 80);
                     } else {
                         // (columns 64..95 held scores that have just been read, columns 0..31 are written behind the reads of theirs)
                         probabilities(v, 64);
