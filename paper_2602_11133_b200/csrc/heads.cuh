@@ -86,27 +86,28 @@ struct HeadArgs {
 
 constexpr int kHeadThreads = 256;
 
-// G lanes per head, two vectors a lane; grid: rows_per_cta rows a CTA.
+// G lanes per head, two vectors a lane; rows_per_cta (a power of two) rows a CTA, each of which has an equal share of the CTA's groups of
+// lanes: a group has one row, so what hangs on the row (cos and sin, gains, slot) is fetched once for all of its heads, and the next
+// head's vectors are requested before the present one's are used.
 template <typename T, int G, bool INTERLEAVED>
-__global__ void __launch_bounds__(kHeadThreads) head_norm_rope_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kHeadThreads, 4) head_norm_rope_kernel(const HeadArgs a) {
     grid_launch_dependents();
     extern __shared__ float2 cs[];                 // [rows_per_cta][half] (cos, sin) times the magnitude
-    const int row0 = blockIdx.x * a.rows_per_cta;
-    const int rows = min(a.rows_per_cta, a.n_rows - row0);
-    const int sub = threadIdx.x % G, group = threadIdx.x / G;
     constexpr int GROUPS = kHeadThreads / G;
+    const int row0 = blockIdx.x * a.rows_per_cta, rows = min(a.rows_per_cta, a.n_rows - row0);
+    const int sub = threadIdx.x % G, group = threadIdx.x / G, per_row = GROUPS / a.rows_per_cta, r = group / per_row;
     const int nvec = a.head_dim / 8, rot = a.half / 8;      // rot: vectors of each half (pairs far apart)
     // the two vectors of this lane, -1 where it has none
     int va, vb;
-    bool turn;
+    bool turn = true, turn_b = true;                        // whether they are turned (each of four whole pairs where pairs are interleaved)
     if (INTERLEAVED) {
         va = 2 * sub < nvec ? 2 * sub : -1;
         vb = 2 * sub + 1 < nvec ? 2 * sub + 1 : -1;
-        turn = true;
+        turn = va >= 0 && va * 4 < a.half;
+        turn_b = vb >= 0 && vb * 4 < a.half;
     } else if (sub < rot) {
         va = sub;
         vb = sub + rot;
-        turn = true;
     } else {
         va = 2 * rot + 2 * (sub - rot);
         vb = va + 1 < nvec ? va + 1 : -1;
@@ -114,41 +115,63 @@ __global__ void __launch_bounds__(kHeadThreads) head_norm_rope_kernel(const Head
         turn = false;
     }
     grid_dependency_wait();
+    const int heads = a.q.n + a.k.n + a.v.n, row = row0 + r;
+    const bool real = r < rows;
+    auto operand = [&](int& h) -> const HeadsDev& {         // of head h of a row's queries, keys and values; h becomes its index among its kind
+        if (h < a.q.n) return a.q;
+        h -= a.q.n;
+        if (h < a.k.n) return a.k;
+        h -= a.k.n;
+        return a.v;
+    };
+    uint4 next_a = make_uint4(0, 0, 0, 0), next_b = next_a;
+    auto request = [&](int h) {
+        if (!real || h >= heads) return;
+        const HeadsDev& x = operand(h);
+        const uint4* src = reinterpret_cast<const uint4*>((const T*)x.in + row * x.in_row + h * x.in_head);
+        if (va >= 0) next_a = src[va];
+        if (vb >= 0) next_b = src[vb];
+    };
+    const int first = group - r * per_row;
+    request(first);
+    const int pos = real ? a.positions[row] : -1;
+    int slot = a.to_pages && real ? a.slots[row] : -1;
     for (int i = threadIdx.x; i < rows * a.half; i += kHeadThreads) {
-        const int pos = a.positions[row0 + i / a.half];
-        const double turns = (double)pos * (double)a.inv_freq[i % a.half] * 0.15915494309189533577;    // 1 / (2 pi)
+        const double turns = (double)a.positions[row0 + i / a.half] * (double)a.inv_freq[i % a.half] * 0.15915494309189533577;    // 1 / (2 pi)
         float s, c;
         sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
         cs[i] = make_float2(c * a.magnitude, s * a.magnitude);
     }
     __syncthreads();
-    const int heads = a.q.n + a.k.n + a.v.n;
-    const unsigned mask = G == 32 ? 0xffffffffu : ((1u << G) - 1u) << (threadIdx.x % 32 / G * G);
-    for (int item = group; item < rows * heads; item += GROUPS) {
-        const int r = item / heads, row = row0 + r;
-        int h = item - r * heads;
-        if (a.positions[row] < 0) continue;
-        const bool is_v = h >= a.q.n + a.k.n, is_k = !is_v && h >= a.q.n;
-        const HeadsDev& x = is_v ? a.v : (is_k ? a.k : a.q);
-        h -= is_v ? a.q.n + a.k.n : (is_k ? a.q.n : 0);
-        T* dst;
-        if ((is_k || is_v) && a.to_pages) {
-            const int slot = a.slots[row];
-            const int page = slot / a.pages.page_size;
-            if (slot < 0) continue;
-            if (page >= a.pages.n_pages) {
-                if (sub == 0 && a.status) atomicExch(a.status, kStatusBadIndex);
-                continue;
-            }
-            const int64_t in_page = ((int64_t)h * a.pages.page_size + (slot - page * a.pages.page_size)) * a.head_dim;
-            dst = is_v ? (T*)a.pages.v + page * a.pages.v_page + in_page : (T*)a.pages.k + page * a.pages.k_page + in_page;
+    if (pos < 0) return;
+    // cos and sin of this lane's pairs: eight, of vectors a and b together
+    float2 t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int i = INTERLEAVED ? (j < 4 ? va * 4 + j : vb * 4 + j - 4) : va * 8 + j;
+        t[j] = (INTERLEAVED && j >= 4 ? turn_b : turn) ? cs[r * a.half + i] : make_float2(1.f, 0.f);
+    }
+    int64_t k_at = 0, v_at = 0;                             // head 0 of the row in its page
+    if (a.to_pages && slot >= 0) {
+        const int page = slot / a.pages.page_size, off = slot - page * a.pages.page_size;
+        if (page >= a.pages.n_pages) {
+            if (group == r * per_row && sub == 0 && a.status) atomicExch(a.status, kStatusBadIndex);
+            slot = -1;
         } else {
-            dst = (T*)x.out + row * x.out_row + h * x.out_head;
+            k_at = page * a.pages.k_page + (int64_t)off * a.head_dim;
+            v_at = page * a.pages.v_page + (int64_t)off * a.head_dim;
         }
-        const T* src = (const T*)x.in + row * x.in_row + h * x.in_head;
-        uint4 ra = make_uint4(0, 0, 0, 0), rb = ra;
-        if (va >= 0) ra = reinterpret_cast<const uint4*>(src)[va];
-        if (vb >= 0) rb = reinterpret_cast<const uint4*>(src)[vb];
+    }
+    const int64_t head_in_page = (int64_t)a.pages.page_size * a.head_dim;
+    const unsigned mask = G == 32 ? 0xffffffffu : ((1u << G) - 1u) << (threadIdx.x % 32 / G * G);
+    for (int item = first; item < heads; item += per_row) {
+        uint4 ra = next_a, rb = next_b;
+        request(item + per_row);
+        int h = item;
+        const HeadsDev& x = operand(h);
+        const bool is_v = item >= a.q.n + a.k.n, to_page = a.to_pages && item >= a.q.n;
+        if (to_page && slot < 0) break;                     // keys and values come last
+        T* dst = to_page ? (is_v ? (T*)a.pages.v + v_at : (T*)a.pages.k + k_at) + h * head_in_page : (T*)x.out + row * x.out_row + h * x.out_head;
         if (!is_v) {
             float fa[8], fb[8];
             unpack8<T>(ra, fa);
@@ -171,31 +194,25 @@ __global__ void __launch_bounds__(kHeadThreads) head_norm_rope_kernel(const Head
 #pragma unroll
                 for (int j = 0; j < 8; ++j) fb[j] *= inv * g[j];
             }
-            const float2* t = cs + r * a.half;
             if (INTERLEAVED) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int ia = va * 4 + j, ib = vb * 4 + j;
-                    if (va >= 0 && ia < a.half) {
-                        const float2 e = t[ia];
-                        const float u = fa[2 * j], w = fa[2 * j + 1];
-                        fa[2 * j] = u * e.x - w * e.y;
-                        fa[2 * j + 1] = w * e.x + u * e.y;
+                    const float u = fa[2 * j], w = fa[2 * j + 1], y = fb[2 * j], z = fb[2 * j + 1];
+                    if (turn) {
+                        fa[2 * j] = u * t[j].x - w * t[j].y;
+                        fa[2 * j + 1] = w * t[j].x + u * t[j].y;
                     }
-                    if (vb >= 0 && ib < a.half) {
-                        const float2 e = t[ib];
-                        const float u = fb[2 * j], w = fb[2 * j + 1];
-                        fb[2 * j] = u * e.x - w * e.y;
-                        fb[2 * j + 1] = w * e.x + u * e.y;
+                    if (turn_b) {
+                        fb[2 * j] = y * t[4 + j].x - z * t[4 + j].y;
+                        fb[2 * j + 1] = z * t[4 + j].x + y * t[4 + j].y;
                     }
                 }
             } else if (turn) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float2 e = t[va * 8 + j];
                     const float u = fa[j], w = fb[j];
-                    fa[j] = u * e.x - w * e.y;
-                    fb[j] = w * e.x + u * e.y;
+                    fa[j] = u * t[j].x - w * t[j].y;
+                    fb[j] = w * t[j].x + u * t[j].y;
                 }
             }
             ra = pack8<T>(fa);

@@ -246,7 +246,7 @@ int jot_head_norm_rope(const jot_heads* q, const jot_heads* k, const jot_rope* r
     if (k) a.k = heads_dev(k);
     a.positions = d_positions; a.inv_freq = rope->d_inv_freq; a.half = rope->rotary_dim / 2; a.magnitude = rope->magnitude; a.eps = eps;
     a.head_dim = head_dim; a.n_rows = n_rows; a.slots = d_slots; a.status = d_status;
-    a.rows_per_cta = std::min(4, std::max(1, n_rows / (4 * di->sms)));
+    a.rows_per_cta = n_rows >= 16 * di->sms ? 4 : (n_rows >= 8 * di->sms ? 2 : 1);
     cudaStream_t st = (cudaStream_t)stream;
     const bool il = rope->interleaved != 0;
     const int pairs = (head_dim / 8 + 1) / 2;                           // lanes a head needs
