@@ -216,6 +216,20 @@ int jot_denoise_step_cached(jot_model* m, const int32_t* d_tokens, int B, int L,
                             const float* d_bump_val, float* d_top1_logit, float* d_top2_logit, float* d_sumexp,
                             int32_t* d_argmax, const jot_sampling* sampling, int32_t* d_sampled, void* stream);
 
+/* The same cache in pages (jot_kv_pages, declared below): rotated keys and values only, wherever the page table says, so that canvases share a
+ * pool, take as much of it as they are long, and can be forked and moved.  Attached in place of the contiguous cache (attaching either
+ * detaches the other; pages = NULL detaches), it is what jot_denoise_step_cached and jot_generate's kv_cache then use, with the same
+ * meaning.  The pages are bf16, of the model's key heads and head_dim, at least n_layers layers; layer l of the model uses layer l.
+ * d_page_table (device int32, row b = sequence b of a call, table_stride elements from row to row, max_pages * page_size >= max_seq) is
+ * read by every pass and may change between them; a page that lies outside the pages is reported as JOT_ERR_ARG.  Pages of positions
+ * that a pass writes (refresh: all; otherwise the block's) must belong to one sequence of the batch only.  The struct is copied; pages,
+ * table and workspace (device, 256-byte aligned, jot_kv_pages_workspace_bytes() long) are borrowed until detached or the model is freed.
+ * Writes a table into the workspace (synchronous). */
+struct jot_kv_pages;
+size_t jot_kv_pages_workspace_bytes(const jot_model_config* cfg, int max_batch, int max_seq);
+int jot_attach_kv_pages(jot_model* m, const struct jot_kv_pages* pages, const int32_t* d_page_table, int64_t table_stride,
+                        int max_pages, void* d_workspace, size_t workspace_bytes);
+
 /* The LM head + statistics part of jot_denoise_step alone, on caller-supplied final hidden states
  * d_hidden [B*L, d] bf16 (already normalised).  Uses only lm_head, vocab, mask_id and d_model of
  * the model.  Same outputs and options as jot_denoise_step. */
@@ -341,7 +355,7 @@ enum { JOT_STATUS_BAD_INDEX = 6 };
 /* Pages of all layers: element (layer, page, head, offset, d) of k lies at
  *   k + layer * k_layer_stride + page * k_page_stride + (head * page_size + offset) * head_dim + d,
  * likewise v.  n_pages * page_size < 2^31.  Two pages never overlap. */
-typedef struct {
+typedef struct jot_kv_pages {
     void *k, *v;
     int64_t k_layer_stride, v_layer_stride, k_page_stride, v_page_stride;
     int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim;

@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libjot.so")
 SOURCES = ["jot.cu", "paged.cu"]
 HEADERS = ["ptx.cuh", "pdl.cuh", "gemm.cuh", "gemm2.cuh", "gemm_slab.cuh", "gemm_stream.cuh", "attention.cuh", "glue.cuh", "accept.cuh",
            "host.cuh", "heads.cuh", "kv_pages.cuh", "paged_attention.cuh",
-           "paged_attention_umma.cuh"]
+           "paged_attention_umma.cuh", "paged.cuh"]
 
 
 def _nvcc() -> str:

@@ -18,11 +18,10 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "paged.cuh"
 #include "pdl.cuh"
 
 namespace jot {
-
-constexpr int32_t kStatusBadIndex = 6;     // a slot, a page or a length outside the pages: skipped or read as zeros
 
 template <typename T> struct Pack2;
 template <typename T> struct PackIsBf16 { static constexpr bool value = false; };

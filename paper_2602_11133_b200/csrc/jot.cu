@@ -23,6 +23,7 @@
 #include "gemm_stream.cuh"
 #include "glue.cuh"
 #include "host.cuh"
+#include "paged.cuh"
 
 using namespace jot;
 
@@ -495,6 +496,16 @@ struct jot_model {
     std::vector<CUtensorMap> kv_tm_qkv3, kv_tm_vt;
     int kv_map_B = -1, kv_map_L = -1;       // geometry the per-layer maps were encoded for
     int kv_valid_B = -1, kv_valid_L = -1;   // geometry of the last refresh (block passes need one)
+    // the same cache in pages instead (caller's memory too): keys and values only, wherever the page table says
+    bool paged = false;
+    jot_kv_pages pages;
+    const int32_t* page_table;
+    int64_t page_table_stride;
+    int page_table_width;
+    float* inv_freq;                        // slices of the pages' workspace
+    int32_t *page_positions, *page_slots, *page_lens;
+    void* page_attn;
+    size_t page_attn_bytes;
     int32_t* h_pinned = nullptr;    // pinned host words for loop control read-back (two 4-word slots, then SeqState)
     cudaEvent_t step_done[2] = {nullptr, nullptr};
     // optional per-kernel-class timing with CUDA events on the launching stream
@@ -657,13 +668,52 @@ int encode_kv_maps(jot_model* m, int B, int L) {
     return JOT_OK;
 }
 
+// Slices of the workspace that goes with attached pages.
+struct PagesLayout {
+    size_t inv_freq, positions, slots, lens, attn, total;
+};
+PagesLayout pages_layout(const jot_model_config* c, int max_batch, int max_seq) {
+    PagesLayout l;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        size_t o = off;
+        off = align_up(off + bytes, 256);
+        return o;
+    };
+    l.inv_freq = take((size_t)c->head_dim / 2 * 4);
+    l.positions = take((size_t)max_batch * max_seq * 4);
+    l.slots = take((size_t)max_batch * max_seq * 4);
+    l.lens = take((size_t)max_batch * 4);
+    l.attn = take(paged_workspace_most((int64_t)max_seq * (c->n_q_heads / c->n_kv_heads), c->head_dim));
+    l.total = off;
+    return l;
+}
+
 // Which rows a pass covers: positions pos0 .. pos0 + Lr - 1 of every sequence; use_cache: the rotated Q/K
 // rows and V^T of every layer live in the attached KV cache instead of the one scratch buffer, so that a
-// later pass over one block finds the rest of the canvas there.
+// later pass over one block finds the rest of the canvas there.  With attached pages the rotated keys and the values live there.
 struct FwdSpan {
     int Lr, pos0;
     bool use_cache;
 };
+
+// A layer between its projections, over pages: the QKV rows of the pass rotated in place, keys and values into the pages, attention of the
+// rows over all of their canvas.
+int attend_pages(jot_model* m, int layer, int B, int Lr, int qkv_cols, cudaStream_t st) {
+    const jot_model_config& c = m->cfg;
+    const int hd = c.head_dim, nq = c.n_q_heads, nkv = c.n_kv_heads, M = B * Lr;
+    const jot_rope rope{m->inv_freq, hd, 0, 1.f};
+    const jot_heads q{m->qkv, qkv_cols, hd, m->qkv, qkv_cols, hd, nullptr, nq}, k{m->qkv + nq * hd, qkv_cols, hd, nullptr, 0, 0, nullptr, nkv},
+        v{m->qkv + (nq + nkv) * hd, qkv_cols, hd, nullptr, 0, 0, nullptr, nkv};
+    {
+        ProfScope ps(m, JOT_PROF_ROPE, st);
+        JOT_TRY(jot_head_norm_rope(&q, &k, &rope, JOT_BF16, M, hd, 0.f, m->page_positions, &v, &m->pages, layer, m->page_slots, m->ctrl, st));
+    }
+    ProfScope ps(m, JOT_PROF_ATTENTION, st);
+    return jot_paged_attention(m->qkv, (int64_t)Lr * qkv_cols, qkv_cols, hd, m->attn, (int64_t)Lr * nq * hd, nq * hd, hd, nullptr, B, Lr, nq, &m->pages, layer,
+                               m->page_table, m->page_table_stride, m->page_table_width, m->page_lens, 1.f / sqrtf((float)hd), m->page_attn,
+                               m->page_attn_bytes, m->ctrl, st);
+}
 
 // Transformer body: tokens [B, L] -> residual stream m->h [B*Lr, d] (before the final norm).
 // B sequences are processed; with seq_map they are the compacted batch (slot -> sequence of d_tokens).
@@ -671,7 +721,7 @@ int forward_body(jot_model* m, const int32_t* d_tokens, int B, int L, cudaStream
                  const FwdSpan* span = nullptr) {
     const jot_model_config& c = m->cfg;
     const int Lr = span ? span->Lr : L, pos0 = span ? span->pos0 : 0;
-    const bool cached = span && span->use_cache;
+    const bool paged = span && span->use_cache && m->paged, cached = span && span->use_cache && !m->paged;
     const int M = B * Lr, d = c.d_model, hd = c.head_dim, nq = c.n_q_heads, nkv = c.n_kv_heads;
     const int qkv_cols = (nq + 2 * nkv) * hd;
     const int Lp = (int)align_up((size_t)L, 8);
@@ -686,6 +736,9 @@ int forward_body(jot_model* m, const int32_t* d_tokens, int B, int L, cudaStream
         launch_k(embed_kernel, dim3(M), dim3(128), 0, st, d_tokens, m->embed, m->h, d, L, seq_map, Lr, pos0, c.vocab, status);
     }
     JOT_TRY(launch_check());
+    if (paged)
+        JOT_TRY(launch_page_rows(m->page_table, m->page_table_stride, B, L, Lr, pos0, m->pages.page_size, m->pages.n_pages, m->page_positions, m->page_slots,
+                                 m->page_lens, status, st));
     bool norm_ready = false;          // true when a fused split-K tail has already written the next norm into m->a
     for (int l = 0; l < c.n_layers; ++l) {
         if (!norm_ready) {
@@ -698,15 +751,16 @@ int forward_body(jot_model* m, const int32_t* d_tokens, int B, int L, cudaStream
             ProfScope ps(m, JOT_PROF_GEMM_QKV, st);
             p.vt = cached ? m->kv_vt[l] : m->vt; p.rope_cs = m->rope_cs; p.L = L; p.Lp = Lp; p.nq = nq; p.nkv = nkv;
             p.hd = hd; p.rows_per_seq = Lr; p.pos0 = pos0;
-            JOT_TRY(run_gemm(m->di, am.a, m->wqkv[l], EPI_QKV, p, st, nullptr, 0, nullptr, am.slab ? &am.xa : nullptr));
+            JOT_TRY(run_gemm(m->di, am.a, m->wqkv[l], paged ? EPI_STORE : EPI_QKV, p, st, nullptr, 0, nullptr, am.slab ? &am.xa : nullptr));
         }
+        if (paged) JOT_TRY(attend_pages(m, l, B, Lr, qkv_cols, st));
         AttnParams ap{};
         ap.B = B; ap.L = L; ap.nq = nq; ap.nkv = nkv; ap.out = m->attn; ap.status = status;
         ap.q_lo = pos0; ap.q_cnt = Lr;
         ap.scale_log2e = 1.4426950408889634f / sqrtf((float)hd);
         const long items = (long)B * nq * ((Lr + 127) / 128);
         dim3 grid((unsigned)(items < m->di->sms ? items : m->di->sms));
-        {
+        if (!paged) {
             ProfScope ps(m, JOT_PROF_ATTENTION, st);
             const CUtensorMap& tq = cached ? m->kv_tm_qkv3[l] : m->tm_qkv3;
             const CUtensorMap& tv = cached ? m->kv_tm_vt[l] : m->tm_vt;
@@ -876,14 +930,15 @@ int check_step_args(const jot_model* m, const void* tokens, int B, int L, int bl
 }
 
 // Status word the kernels set: 0 ok; kStatusBadToken: a token id outside the vocabulary (the row was embedded as
-// token 0); anything else: a bounded wait expired.
-int status_code(int32_t w) { return w == 0 ? JOT_OK : (w == kStatusBadToken ? JOT_ERR_ARG : JOT_ERR_TIMEOUT); }
+// token 0); kStatusBadIndex: a page of the table outside the pages; anything else: a bounded wait expired.
+bool status_of_input(int32_t w) { return w == kStatusBadToken || w == kStatusBadIndex; }
+int status_code(int32_t w) { return w == 0 ? JOT_OK : (status_of_input(w) ? JOT_ERR_ARG : JOT_ERR_TIMEOUT); }
 
 int read_status(jot_model* m, cudaStream_t st) {
     JOT_CUDA(cudaMemcpyAsync(m->h_pinned, m->ctrl, 4, cudaMemcpyDeviceToHost, st));
     JOT_CUDA(cudaStreamSynchronize(st));
     const int32_t w = m->h_pinned[0];
-    if (w == kStatusBadToken) JOT_CUDA(cudaMemsetAsync(m->ctrl, 0, 4, st));     // the caller can fix its input and go on
+    if (status_of_input(w)) JOT_CUDA(cudaMemsetAsync(m->ctrl, 0, 4, st));     // the caller can fix its input and go on
     return status_code(w);
 }
 
@@ -1149,6 +1204,7 @@ size_t jot_kv_cache_bytes(const jot_model_config* cfg, int max_batch, int max_se
 int jot_attach_kv_cache(jot_model* m, void* d_cache, size_t bytes) {
     if (!m) return JOT_ERR_ARG;
     m->kv_map_B = m->kv_map_L = m->kv_valid_B = m->kv_valid_L = -1;
+    m->paged = false;
     m->kv_base = nullptr;
     m->kv_bytes = 0;
     if (!d_cache) return JOT_OK;                                   // detach
@@ -1168,11 +1224,46 @@ int jot_attach_kv_cache(jot_model* m, void* d_cache, size_t bytes) {
     return JOT_OK;
 }
 
+size_t jot_kv_pages_workspace_bytes(const jot_model_config* cfg, int max_batch, int max_seq) {
+    if (!config_ok(cfg) || max_batch <= 0 || max_seq <= 0) return 0;
+    return pages_layout(cfg, max_batch, max_seq).total;
+}
+
+int jot_attach_kv_pages(jot_model* m, const jot_kv_pages* pages, const int32_t* d_page_table, int64_t table_stride, int max_pages, void* d_workspace,
+                        size_t workspace_bytes) {
+    if (!m) return JOT_ERR_ARG;
+    if (!pages) return jot_attach_kv_cache(m, nullptr, 0);         // detach
+    const jot_model_config& c = m->cfg;
+    JOT_TRY(check_kv_pages(pages, 0));
+    if (!d_page_table || table_stride < 0) return JOT_ERR_ARG;
+    if (pages->dtype != JOT_BF16 || pages->head_dim != c.head_dim || pages->n_kv_heads != c.n_kv_heads || pages->n_layers < c.n_layers) return JOT_ERR_ARG;
+    if (max_pages <= 0 || (int64_t)max_pages * pages->page_size < m->max_seq) return JOT_ERR_SHAPE;
+    const PagesLayout l = pages_layout(&c, m->max_batch, m->max_seq);
+    if (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255) || workspace_bytes < l.total) return JOT_ERR_WORKSPACE;
+    JOT_TRY(jot_attach_kv_cache(m, nullptr, 0));
+    uint8_t* base = (uint8_t*)d_workspace;
+    float freq[64];
+    for (int j = 0; j < c.head_dim / 2; ++j) freq[j] = (float)std::pow((double)c.rope_theta, -2.0 * j / c.head_dim);
+    m->inv_freq = (float*)(base + l.inv_freq);
+    JOT_CUDA(cudaMemcpy(m->inv_freq, freq, (size_t)c.head_dim / 2 * 4, cudaMemcpyHostToDevice));
+    m->page_positions = (int32_t*)(base + l.positions);
+    m->page_slots = (int32_t*)(base + l.slots);
+    m->page_lens = (int32_t*)(base + l.lens);
+    m->page_attn = base + l.attn;
+    m->page_attn_bytes = l.total - l.attn;
+    m->pages = *pages;
+    m->page_table = d_page_table;
+    m->page_table_stride = table_stride;
+    m->page_table_width = max_pages;
+    m->paged = true;
+    return JOT_OK;
+}
+
 int jot_denoise_step_cached(jot_model* m, const int32_t* d_tokens, int B, int L, int blk_lo, int blk_hi, int refresh,
                             int exclude_mask_token, const int32_t* d_bump_id, const float* d_bump_val, float* d_top1,
                             float* d_top2, float* d_sumexp, int32_t* d_argmax, const jot_sampling* sampling,
                             int32_t* d_sampled, void* stream) {
-    if (!m || !m->kv_base) return JOT_ERR_ARG;
+    if (!m || !(m->kv_base || m->paged)) return JOT_ERR_ARG;
     if (blk_lo >= blk_hi) return JOT_ERR_ARG;
     if (!refresh && (m->kv_valid_B != B || m->kv_valid_L != L)) return JOT_ERR_ARG;     // nothing cached for this canvas
     const FwdSpan span = refresh ? FwdSpan{L, 0, true} : FwdSpan{blk_hi - blk_lo, blk_lo, true};
@@ -1272,7 +1363,7 @@ int jot_generate(jot_model* m, const jot_params* params, int per_seq_params, con
         // canvas and leaves every layer's keys and values in the cache; the block's other steps run only the
         // block's rows against it.  The host reads the block's outcome after every step (what runs next depends
         // on it), so this loop is not pipelined.
-        if (!m->kv_base) return JOT_ERR_ARG;
+        if (!m->kv_base && !m->paged) return JOT_ERR_ARG;
         const int Lb = gen->block_len;
         int n_passes = 0;
         for (int blk = 0; blk < nb; ++blk) {
@@ -1303,7 +1394,7 @@ int jot_generate(jot_model* m, const jot_params* params, int per_seq_params, con
                 JOT_CUDA(cudaStreamSynchronize(st));
                 if (m->h_pinned[0]) {
                     const int32_t w0 = m->h_pinned[0];
-                    if (w0 == kStatusBadToken) cudaMemsetAsync(m->ctrl, 0, 4, st);
+                    if (status_of_input(w0)) cudaMemsetAsync(m->ctrl, 0, 4, st);
                     return status_code(w0);
                 }
                 ++n_passes;

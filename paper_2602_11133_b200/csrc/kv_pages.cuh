@@ -40,6 +40,20 @@ __global__ void __launch_bounds__(kMoveThreads) kv_write_kernel(const WriteArgs 
     }
 }
 
+__global__ void page_rows_kernel(const int32_t* __restrict__ table, int64_t table_stride, int B, int L, int rows_per_seq, int pos0, int page_size, int n_pages,
+                                 int32_t* __restrict__ positions, int32_t* __restrict__ slots, int32_t* __restrict__ lens, int32_t* status) {
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int r = blockIdx.x * blockDim.x + threadIdx.x;
+    if (r < B) lens[r] = L;
+    if (r >= B * rows_per_seq) return;
+    const int b = r / rows_per_seq, pos = pos0 + r - b * rows_per_seq, p = pos / page_size, page = table[b * table_stride + p];
+    positions[r] = pos;
+    const bool real = (unsigned)page < (unsigned)n_pages;
+    slots[r] = real ? page * page_size + pos - p * page_size : -1;
+    if (!real) atomicExch(status, kStatusBadIndex);
+}
+
 // The pairs travel as kernel arguments, as the caller's lists live on the host and may change right after the call.
 template <int N>
 struct PagePairs {

@@ -24,21 +24,6 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 // A stride counts only where there is a second element along it.
 bool stride_ok(int64_t s, int64_t n) { return n <= 1 || s % 8 == 0; }
 
-int check_pages(const jot_kv_pages* p, int layer) {
-    if (!p || !p->k || !p->v || !aligned16(p->k) || !aligned16(p->v)) return JOT_ERR_ARG;
-    if (p->n_layers <= 0 || p->n_pages <= 0 || p->n_kv_heads <= 0 || p->page_size <= 0 || p->head_dim <= 0) return JOT_ERR_ARG;
-    if (layer < 0 || layer >= p->n_layers) return JOT_ERR_ARG;
-    if (p->dtype != JOT_BF16 && p->dtype != JOT_FP16) return JOT_ERR_ARG;
-    if (p->head_dim % 8 || (int64_t)p->n_pages * p->page_size > INT32_MAX) return JOT_ERR_SHAPE;
-    const int64_t page = (int64_t)p->n_kv_heads * p->page_size * p->head_dim;
-    if (page / 8 > INT32_MAX / 2) return JOT_ERR_SHAPE;
-    if (!stride_ok(p->k_layer_stride, p->n_layers) || !stride_ok(p->v_layer_stride, p->n_layers) ||
-        !stride_ok(p->k_page_stride, p->n_pages) || !stride_ok(p->v_page_stride, p->n_pages))
-        return JOT_ERR_ARG;
-    if (p->n_pages > 1 && (std::abs(p->k_page_stride) < page || std::abs(p->v_page_stride) < page)) return JOT_ERR_ARG;
-    return JOT_OK;
-}
-
 PagesDev layer_pages(const jot_kv_pages* p, int layer) {
     return PagesDev{(uint16_t*)p->k + layer * p->k_layer_stride, (uint16_t*)p->v + layer * p->v_layer_stride, p->k_page_stride,
                     p->v_page_stride, p->n_pages, p->page_size};
@@ -217,6 +202,41 @@ int launch_paged(const DeviceInfo* di, const PagedArgs& a, int row_tile, cudaStr
 
 }  // namespace
 
+namespace jot {
+
+int check_kv_pages(const jot_kv_pages* p, int layer) {
+    if (!p || !p->k || !p->v || !aligned16(p->k) || !aligned16(p->v)) return JOT_ERR_ARG;
+    if (p->n_layers <= 0 || p->n_pages <= 0 || p->n_kv_heads <= 0 || p->page_size <= 0 || p->head_dim <= 0) return JOT_ERR_ARG;
+    if (layer < 0 || layer >= p->n_layers) return JOT_ERR_ARG;
+    if (p->dtype != JOT_BF16 && p->dtype != JOT_FP16) return JOT_ERR_ARG;
+    if (p->head_dim % 8 || (int64_t)p->n_pages * p->page_size > INT32_MAX) return JOT_ERR_SHAPE;
+    const int64_t page = (int64_t)p->n_kv_heads * p->page_size * p->head_dim;
+    if (page / 8 > INT32_MAX / 2) return JOT_ERR_SHAPE;
+    if (!stride_ok(p->k_layer_stride, p->n_layers) || !stride_ok(p->v_layer_stride, p->n_layers) ||
+        !stride_ok(p->k_page_stride, p->n_pages) || !stride_ok(p->v_page_stride, p->n_pages))
+        return JOT_ERR_ARG;
+    if (p->n_pages > 1 && (std::abs(p->k_page_stride) < page || std::abs(p->v_page_stride) < page)) return JOT_ERR_ARG;
+    return JOT_OK;
+}
+
+int launch_page_rows(const int32_t* table, int64_t table_stride, int B, int L, int rows_per_seq, int pos0, int page_size, int n_pages, int32_t* positions,
+                     int32_t* slots, int32_t* lens, int32_t* status, cudaStream_t st) {
+    launch_k(page_rows_kernel, dim3((unsigned)((std::max(B, B * rows_per_seq) + 255) / 256)), dim3(256), 0, st, table, table_stride, B, L, rows_per_seq, pos0, page_size,
+             n_pages, positions, slots, lens, status);
+    return launch_check();
+}
+
+size_t paged_workspace_most(int64_t max_rows, int head_dim) {
+    size_t most = 0;
+    for (int tile : {16, 32, 64, 128, 256}) {
+        most = std::max(most, paged_space(tile, head_dim).total);
+        if (tile >= max_rows) break;
+    }
+    return most;
+}
+
+}  // namespace jot
+
 extern "C" {
 
 int jot_head_norm_rope(const jot_heads* q, const jot_heads* k, const jot_rope* rope, int dtype, int n_rows, int head_dim, float eps,
@@ -234,7 +254,7 @@ int jot_head_norm_rope(const jot_heads* q, const jot_heads* k, const jot_rope* r
     HeadArgs a{};
     if (pages) {
         JOT_TRY(check_heads(v, n_rows, false));
-        JOT_TRY(check_pages(pages, layer));
+        JOT_TRY(check_kv_pages(pages, layer));
         if (pages->dtype != dtype || pages->head_dim != head_dim || pages->n_kv_heads != k->n_heads || v->n_heads != k->n_heads) return JOT_ERR_ARG;
         a.pages = layer_pages(pages, layer);
         a.to_pages = 1;
@@ -260,7 +280,7 @@ int jot_head_norm_rope(const jot_heads* q, const jot_heads* k, const jot_rope* r
 
 int jot_kv_write(const jot_kv_pages* pages, int layer, int n_rows, const void* d_k, int64_t k_row_stride, int64_t k_head_stride,
                  const void* d_v, int64_t v_row_stride, int64_t v_head_stride, const int32_t* d_slots, int32_t* d_status, void* stream) {
-    JOT_TRY(check_pages(pages, layer));
+    JOT_TRY(check_kv_pages(pages, layer));
     if (n_rows == 0) return JOT_OK;
     if (!d_k || !d_v || !d_slots || n_rows < 0 || !aligned16(d_k) || !aligned16(d_v)) return JOT_ERR_ARG;
     if (!stride_ok(k_row_stride, n_rows) || !stride_ok(v_row_stride, n_rows) || !stride_ok(k_head_stride, pages->n_kv_heads) ||
@@ -280,7 +300,7 @@ int jot_kv_write(const jot_kv_pages* pages, int layer, int n_rows, const void* d
 }
 
 int jot_kv_copy_pages(const jot_kv_pages* pages, int n, const int32_t* src, const int32_t* dst, void* stream) {
-    JOT_TRY(check_pages(pages, 0));
+    JOT_TRY(check_kv_pages(pages, 0));
     if (n < 0 || (n > 0 && (!src || !dst))) return JOT_ERR_ARG;
     JOT_TRY(check_moves(pages->n_pages, n, src, dst));
     CopyArgs a{};
@@ -313,7 +333,7 @@ int jot_paged_attention(const void* d_q, int64_t q_seq_stride, int64_t q_row_str
                         int64_t out_seq_stride, int64_t out_row_stride, int64_t out_head_stride, float* d_lse, int B, int T, int n_q_heads,
                         const jot_kv_pages* pages, int layer, const int32_t* d_page_table, int64_t table_stride, int max_pages,
                         const int32_t* d_lens, float scale, void* d_workspace, size_t workspace_bytes, int32_t* d_status, void* stream) {
-    JOT_TRY(check_pages(pages, layer));
+    JOT_TRY(check_kv_pages(pages, layer));
     if (B < 0 || T < 0 || n_q_heads <= 0 || max_pages < 0 || table_stride < 0) return JOT_ERR_ARG;
     if (B == 0 || T == 0) return JOT_OK;
     if (!d_q || !d_out || !d_lens || (max_pages > 0 && !d_page_table) || !aligned16(d_q) || !aligned16(d_out)) return JOT_ERR_ARG;

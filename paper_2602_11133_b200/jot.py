@@ -25,7 +25,7 @@ EXPORTS = [
     "jot_selftest_wait_expiry", "jot_kv_cache_bytes", "jot_attach_kv_cache", "jot_denoise_step_cached",
     "jot_max_active_rows", "jot_lm_head_partition", "jot_set_sync", "jot_read_status",
     "jot_lm_head_stats_slice", "jot_merge_stats", "jot_head_norm_rope", "jot_kv_write", "jot_kv_copy_pages",
-    "jot_paged_attention", "jot_paged_attention_workspace_bytes",
+    "jot_paged_attention", "jot_paged_attention_workspace_bytes", "jot_kv_pages_workspace_bytes", "jot_attach_kv_pages",
 ]
 
 NOALLOC_SCRATCH_BYTES = 16 << 20
@@ -167,6 +167,9 @@ def _lib():
         lib.jot_kv_write.argtypes = [pages, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64,
                                      C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
         lib.jot_kv_copy_pages.argtypes = [pages, C.c_int, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_void_p]
+        lib.jot_kv_pages_workspace_bytes.restype = C.c_size_t
+        lib.jot_kv_pages_workspace_bytes.argtypes = [C.POINTER(ModelConfig), C.c_int, C.c_int]
+        lib.jot_attach_kv_pages.argtypes = [C.c_void_p, pages, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_size_t]
         lib.jot_paged_attention_workspace_bytes.restype = C.c_size_t
         lib.jot_paged_attention_workspace_bytes.argtypes = [C.c_int] * 4
         lib.jot_paged_attention.argtypes = ([C.c_void_p, C.c_int64, C.c_int64, C.c_int64] * 2 + [C.c_void_p] + [C.c_int] * 3
@@ -284,6 +287,21 @@ class Model:
     def detach_kv_cache(self) -> None:
         _check(_lib().jot_attach_kv_cache(self.handle, None, 0), "jot_attach_kv_cache")
         self.kv_cache = None
+
+    def attach_kv_pages(self, pages: "KVPages", page_table: torch.Tensor) -> None:
+        """The block-wise cache in the caller's pages: page_table [max_batch, max_pages] int32, read by every pass (it may
+        change between them).  Takes the place of an attached contiguous cache; detach_kv_cache detaches it."""
+        dev = self.workspace.device
+        if pages.device != dev or page_table.device != dev or page_table.dtype != torch.int32 or page_table.dim() != 2 or (
+                page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise TypeError(f"attach_kv_pages: expected pages and an int32 table with contiguous rows on {dev}")
+        if page_table.shape[0] < self.max_batch:
+            raise ValueError(f"attach_kv_pages: the table has {page_table.shape[0]} rows, the model takes {self.max_batch} sequences")
+        nbytes = _lib().jot_kv_pages_workspace_bytes(C.byref(self.cfg), self.max_batch, self.max_seq)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        _check(_lib().jot_attach_kv_pages(self.handle, pages._ref, page_table.data_ptr(), page_table.stride(0), page_table.shape[1],
+                                          workspace.data_ptr(), nbytes), "jot_attach_kv_pages")
+        self.kv_cache = (pages, page_table, workspace)       # keep them alive
 
     def denoise_step_cached(self, tokens: torch.Tensor, blk_lo: int, blk_hi: int, refresh: bool,
                             out: Optional["Stats"] = None, exclude_mask_token: bool = True,
