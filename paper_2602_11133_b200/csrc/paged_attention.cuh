@@ -135,7 +135,7 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
     int in_seq = 0;
     const int first = tiles_of(a.B <= 32 ? lane : tid);
     auto cut = [](int total, int stream, int& begin, int& end) {
-        const int ctas = min((int)gridDim.x * STREAMS, total), i = blockIdx.x * STREAMS + stream;
+        const int ctas = min((int)gridDim.x * STREAMS, total), i = stream * gridDim.x + blockIdx.x;
         begin = i < ctas ? paged_share(total, ctas, i) : 0;
         end = i < ctas ? paged_share(total, ctas, i + 1) : 0;
         return ctas;

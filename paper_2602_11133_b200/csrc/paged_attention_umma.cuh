@@ -180,8 +180,8 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     // the stream of this warp (TWO: 0 for the producers, who serve both)
     const int s = warp < 8 ? warp >> 2 : (warp >= Role::MMA ? warp - Role::MMA : (TWO ? 0 : (warp - Role::PROD) / Role::PROD_WARPS));
     const PagedRange rg = paged_range<T, HD, THREADS, STREAMS>(a, KEYS, per_b, TWO ? 0 : s, range_smem);
-    const int share = blockIdx.x * STREAMS + (TWO ? 0 : s);
-    if (tid < STREAMS) a.desc[blockIdx.x * STREAMS + tid] = make_int4(0, 0, 0, 0);
+    const int share = (TWO ? 0 : s) * gridDim.x + blockIdx.x;      // first one for every CTA, then a second
+    if (tid < STREAMS) a.desc[tid * gridDim.x + blockIdx.x] = make_int4(0, 0, 0, 0);
     __syncthreads();                             // (a descriptor is written again below)
     auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {
         const bool w = mbar_wait(bar, parity, abortp);
