@@ -109,6 +109,9 @@ int launch_join(const PagedArgs& a, int grid, int row_tile, cudaStream_t st) {
     return launch_check();
 }
 
+// Up to so many tiles (of what a table row has room for) an item is not cut: the second kernel and the parts' way through memory cost more.
+// One row over 129 keys 23.4 -> 22 us a call, 384 rows over 384 keys 28.7 -> 24 us (the library's two launches are 2.5 us of a call's time).
+constexpr int kPagedWhole = 4;
 // What the table can hold bounds the line of tiles: of an item, and of them all (no more than there may be CTAs).
 int64_t paged_tiles(const PagedArgs& a, int keys) { return ((int64_t)a.max_pages * a.pages.page_size + keys - 1) / keys; }
 int64_t paged_most(const PagedArgs& a, int64_t items, int64_t tiles) {
@@ -117,7 +120,7 @@ int64_t paged_most(const PagedArgs& a, int64_t items, int64_t tiles) {
 }
 
 template <typename T, int HD, int WM>
-int launch_paged_t(const DeviceInfo* di, const PagedArgs& a, int64_t items, cudaStream_t st) {
+int launch_paged_t(const DeviceInfo* di, PagedArgs a, int64_t items, cudaStream_t st) {
     static thread_local int per_sm[64] = {};
     int dev = 0;
     JOT_CUDA(cudaGetDevice(&dev));
@@ -132,10 +135,11 @@ int launch_paged_t(const DeviceInfo* di, const PagedArgs& a, int64_t items, cuda
         occ = n;
     }
     const int64_t tiles = paged_tiles(a, kPagedTile);
+    a.whole = tiles <= kPagedWhole;
     const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(occ * di->sms, kPagedMaxCtas));
     launch_k(kernel, dim3((unsigned)grid), dim3(kPagedThreads), smem, st, a);
     JOT_TRY(launch_check());
-    return tiles <= 1 ? JOT_OK : launch_join<T, HD>(a, grid, 16 * WM, st);     // an item of one tile is never in two CTAs
+    return a.whole ? JOT_OK : launch_join<T, HD>(a, grid, 16 * WM, st);
 }
 
 // (head_dim, key of the page, head, page); a box is 64 columns of a page's keys, or of 128 of them.  Out-of-range pages read as zeros.
@@ -180,14 +184,16 @@ int launch_paged_umma_t(const DeviceInfo* di, const PagedArgs& a, int grid, cuda
 }
 
 template <typename T, int HD, int ROWS>
-int launch_paged_umma(const DeviceInfo* di, const PagedArgs& a, int64_t items, cudaStream_t st) {
+int launch_paged_umma(const DeviceInfo* di, PagedArgs a, int64_t items, cudaStream_t st) {
     const bool tma = paged_tma_pages(a.pages.page_size) && a.pages.k_page >= 0 && a.pages.v_page >= 0;
     const int64_t tiles = paged_tiles(a, tma ? paged_tma_keys(a.pages.page_size) : kUmmaPagedTile);
     constexpr int streams = ROWS == 256 ? 1 : 2;
-    const int grid = (int)std::min<int64_t>((paged_most(a, items, tiles) + streams - 1) / streams, std::min(di->sms, kUmmaPagedMaxCtas));
+    // two tiles of rows take twice as long over a tile of keys: worth cutting unless a third of the SMs have items of their own
+    a.whole = tiles <= 1 || (tiles <= kPagedWhole && (ROWS < 256 || 3 * items * a.B >= di->sms));
+    const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(di->sms, kUmmaPagedMaxCtas));
     if (tma) JOT_TRY((launch_paged_umma_t<T, HD, ROWS, true>(di, a, grid, st)));
     else JOT_TRY((launch_paged_umma_t<T, HD, ROWS, false>(di, a, grid, st)));
-    return tiles <= 1 ? JOT_OK : launch_join<T, HD>(a, grid * streams, ROWS, st);
+    return a.whole ? JOT_OK : launch_join<T, HD>(a, grid * streams, ROWS, st);
 }
 
 template <typename T, int HD>

@@ -10,7 +10,8 @@
 // of any and unequal length, known on the device only, so the work is cut there: all tiles of 64 keys of all (sequence, key
 // head, row tile) items form one line, and CTA i of G takes the tiles [i W / G, (i + 1) W / G) of it, whatever items they belong
 // to.  An item that lies in one CTA's range is finished there; one that spans several leaves, per CTA, the unnormalised fp32
-// output with its maximum and sum, which a second kernel joins.  Nothing is added with atomics: a call gives the same bits every time.
+// output with its maximum and sum, which a second kernel joins.  Where a table row has room for a few tiles only, items are not cut and
+// there is no second kernel.  Nothing is added with atomics: a call gives the same bits every time.
 //
 // A CTA keeps three stages of 64 keys in flight (cp.async, 16 bytes a request, a page table entry fetched one tile ahead); its four
 // warps share a stage as WM warps of 16 rows by 4 / WM ranges of keys, and each range keeps a maximum, a sum and an accumulator of
@@ -45,6 +46,7 @@ struct PagedArgs {
     int max_pages;
     const int32_t* lens;                    // [B]; 0: zeros come out; negative: the sequence's rows stay as they were
     float scale_log2;                       // scale * log2(e)
+    bool whole;                             // items are not cut: shares are whole items, and nothing is left to join
     // workspace: one descriptor per CTA, then two partial results per CTA
     int4* desc;                             // (sequence, item within it, fragments, -) of the item that begins in CTA i and ends in a later one
     float* partial;                         // [CTA][2][MT][HD] unnormalised outputs
@@ -121,7 +123,7 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
         const int n = paged_len(a, b);
         empty |= n == 0;
         if (blockIdx.x == 0 && a.status && a.lens[b] > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
-        return n > 0 ? (n + tile - 1) / tile * per_b : 0;
+        return n > 0 ? (a.whole ? per_b : (n + tile - 1) / tile * per_b) : 0;
     };
     auto scan = [&](int v) {        // inclusive, over the warp
 #pragma unroll
@@ -191,8 +193,21 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
     if (rg.end > rg.begin) {
         rg.n = paged_len(a, rg.b);
         const int nt = (rg.n + tile - 1) / tile;
-        rg.item = in_seq / nt;
-        rg.kt = in_seq - rg.item * nt;
+        rg.item = a.whole ? in_seq : in_seq / nt;
+        rg.kt = a.whole ? 0 : in_seq - rg.item * nt;
+        if (a.whole) {              // a share of items so far: how many tiles that is
+            int left = rg.end - rg.begin, tiles = 0;
+            for (int b = rg.b, from = rg.item; left > 0; ++b) {
+                const int n = paged_len(a, b);
+                if (n <= 0) continue;
+                const int items = min(per_b - from, left);
+                tiles += items * ((n + tile - 1) / tile);
+                left -= items;
+                from = 0;
+            }
+            rg.begin = 0;
+            rg.end = tiles;
+        }
     }
     for (int b = blockIdx.x; empty && b < a.B; b += gridDim.x) {
         if (paged_len(a, b) != 0) continue;

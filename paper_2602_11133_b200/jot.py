@@ -608,11 +608,13 @@ def rope_frequencies(rotary_dim: int, theta: float, factor: float = 1.0, origina
     return (f * (keep + (1.0 - keep) / factor)).to(torch.float32).to(device)
 
 
-def _heads(x: torch.Tensor, out: Optional[torch.Tensor], gain: Optional[torch.Tensor], name: str, device, dtype, rows: int, hd: int) -> _Heads:
+def _heads(x: torch.Tensor, out: Optional[torch.Tensor], gain: Optional[torch.Tensor], name: str, device, dtype, rows: int, hd: int,
+           fresh: bool = False) -> _Heads:
+    """fresh: out was made here, like x."""
     n = x.shape[1]
     shape = (rows, n, hd)
     xs = _element_strides(x, name, dtype, device, shape)
-    outs = (0, 0) if out is None else _element_strides(out, name + "_out", dtype, device, shape)
+    outs = (0, 0) if out is None else out.stride() if fresh else _element_strides(out, name + "_out", dtype, device, shape)
     if gain is not None and (gain.dtype != dtype or gain.device != device or gain.dim() != 1 or gain.numel() != hd or not gain.is_contiguous()):
         raise TypeError(f"{name}_gain: expected a contiguous {dtype} tensor [{hd}] on {device}")
     return _Heads(x.data_ptr(), xs[0], xs[1], None if out is None else out.data_ptr(), outs[0], outs[1], None if gain is None else gain.data_ptr(), n)
@@ -637,7 +639,8 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.
     if f.dtype != torch.float32 or f.device != device or f.dim() != 1 or not f.is_contiguous():
         raise TypeError(f"rope.inv_freq: expected a contiguous 1-D float32 tensor on {device}")
     hk = hv = ref = None
-    if q_out is None:
+    fresh_q, fresh_k = q_out is None, k_out is None
+    if fresh_q:
         q_out = torch.empty_like(q)
     if pages is None:
         if v is not None or slots is not None:
@@ -645,7 +648,7 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.
         if k is not None:
             if k_out is None:
                 k_out = torch.empty_like(k)
-            hk = C.byref(_heads(k, k_out, k_gain, "k", device, dtype, rows, hd))
+            hk = C.byref(_heads(k, k_out, k_gain, "k", device, dtype, rows, hd, fresh_k))
     else:
         if k is None or v is None or slots is None or k_out is not None:
             raise ValueError("head_norm_rope: pages need k, v and slots, and take the place of k_out")
@@ -654,7 +657,7 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.
         ref = pages._ref
         hk = C.byref(_heads(k, None, k_gain, "k", device, dtype, rows, hd))
         hv = C.byref(_heads(v, None, None, "v", device, dtype, rows, hd))
-    _launch(device, "jot_head_norm_rope", _lib().jot_head_norm_rope, C.byref(_heads(q, q_out, q_gain, "q", device, dtype, rows, hd)), hk,
+    _launch(device, "jot_head_norm_rope", _lib().jot_head_norm_rope, C.byref(_heads(q, q_out, q_gain, "q", device, dtype, rows, hd, fresh_q)), hk,
             C.byref(_Rope(f.data_ptr(), 2 * f.numel(), rope.interleaved, rope.magnitude)), _ELEMENTS[dtype], rows, hd, eps,
             _int_ptr(positions, "positions", device, rows), hv, ref, layer, _int_ptr(slots, "slots", device, rows),
             _int_ptr(status, "status", device, 1))
@@ -703,7 +706,9 @@ def paged_attention(q: torch.Tensor, pages: KVPages, page_table: torch.Tensor, l
     qs = _element_strides(q, "q", pages.dtype, device, shape)
     if out is None:
         out = torch.empty_like(q)
-    outs = _element_strides(out, "out", pages.dtype, device, shape)
+        outs = out.stride()
+    else:
+        outs = _element_strides(out, "out", pages.dtype, device, shape)
     if lse is not None and (lse.dtype != torch.float32 or lse.device != device or lse.shape != shape[:3] or not lse.is_contiguous()):
         raise TypeError(f"lse: expected a contiguous float32 tensor {tuple(shape[:3])} on {device}")
     table = page_table.shape

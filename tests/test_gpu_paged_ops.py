@@ -273,6 +273,8 @@ ATTENTION_CASES = [
     (33, 2, 2, 64, 56, FP16, [112, 113, 500]),              # tiles of two pages with room behind them
     (18, 1, 1, 128, 120, BF16, [121, 240]),
     (20, 4, 4, 64, 200, BF16, [401, 77]),
+    (1, 8, 2, 128, 16, BF16, [(i * 29) % 190 - 3 for i in range(100)]),     # tables of few tiles: sequences are not cut
+    (40, 8, 2, 64, 64, BF16, [(i * 71) % 250 for i in range(50)]),
 ]
 
 
