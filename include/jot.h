@@ -347,7 +347,8 @@ int jot_gemm_bf16_noalloc(const void* d_A, const void* d_W, const void* d_residu
  *   - A negative position, slot or length marks padding: what belongs to it stays as it was.
  *   - Slots, page numbers and lengths live on the device and are checked there: what lies outside the pages is never
  *     read or written (a slot is skipped; a page reads as zeros; a length counts up to the end of the table's row), and
- *     *d_status (int32, nullable, never reset) becomes JOT_STATUS_BAD_INDEX.
+ *     *d_status (int32, nullable, never reset) becomes JOT_STATUS_BAD_INDEX.  (2 there: a bounded wait on the device expired; the
+ *     call's outputs are undefined.)
  *   - Nothing is allocated and nothing synchronises; the calls may be captured into a CUDA graph. */
 enum { JOT_BF16 = 0, JOT_FP16 = 1 };
 enum { JOT_STATUS_BAD_INDEX = 6 };
@@ -407,7 +408,8 @@ int jot_kv_copy_pages(const jot_kv_pages* pages, int n, const int32_t* src, cons
  * d_page_table[b * table_stride + j / page_size] at offset j % page_size, j < d_lens[b].  Every row sees every key
  * (bidirectional).  q and out [B, T, n_q_heads, head_dim] with strides (sequence, row, head); query head h uses key head
  * h / (n_q_heads / n_kv_heads).  d_lse (nullable, [B, T, n_q_heads] fp32): ln of the sum of exp(scale * q . k).  A length of 0
- * gives zeros and -inf.  head_dim 64 or 128.  Entries of a table row past its length are not read.  Tokens past a length within
+ * gives zeros and -inf.  head_dim 64 or 128.  Fewer than 2^31 tiles of 64 keys over all sequences, heads and rows, were every
+ * sequence as long as its table row allows.  Entries of a table row past its length are not read.  Tokens past a length within
  * a page may hold anything, NaN included.
  * d_workspace: at least jot_paged_attention_workspace_bytes() (0 on invalid arguments), 16-byte aligned, the call's own until it
  * has finished on the device: two calls (or two graphs) that may run at the same time need one each. */

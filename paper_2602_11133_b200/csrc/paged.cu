@@ -110,7 +110,7 @@ int launch_join(const PagedArgs& a, int grid, int row_tile, cudaStream_t st) {
 }
 
 // Up to so many tiles (of what a table row has room for) an item is not cut: the second kernel and the parts' way through memory cost more.
-// One row over 129 keys 23.4 -> 22 us a call, 384 rows over 384 keys 28.7 -> 24 us (the library's two launches are 2.5 us of a call's time).
+// One row over 129 keys 23.4 -> 21.6 us a call (half of it the caller's side of two launches), 384 rows of 32 heads over 384 keys 28.7 -> 16.3 us.
 constexpr int kPagedWhole = 4;
 // What the table can hold bounds the line of tiles: of an item, and of them all (no more than there may be CTAs).
 int64_t paged_tiles(const PagedArgs& a, int keys) { return ((int64_t)a.max_pages * a.pages.page_size + keys - 1) / keys; }
@@ -119,13 +119,13 @@ int64_t paged_most(const PagedArgs& a, int64_t items, int64_t tiles) {
     return std::max<int64_t>(1, std::min<int64_t>(kPagedMaxCtas, n) * std::min<int64_t>(tiles, kPagedMaxCtas));
 }
 
-template <typename T, int HD, int WM>
+template <typename T, int HD>
 int launch_paged_t(const DeviceInfo* di, PagedArgs a, int64_t items, cudaStream_t st) {
     static thread_local int per_sm[64] = {};
     int dev = 0;
     JOT_CUDA(cudaGetDevice(&dev));
     int& occ = per_sm[dev & 63];
-    auto* kernel = paged_attention_kernel<T, HD, WM>;
+    auto* kernel = paged_attention_kernel<T, HD>;
     constexpr int smem = PagedSmem<HD>::DYN_BYTES;
     if (occ == 0) {
         JOT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
@@ -139,7 +139,7 @@ int launch_paged_t(const DeviceInfo* di, PagedArgs a, int64_t items, cudaStream_
     const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(occ * di->sms, kPagedMaxCtas));
     launch_k(kernel, dim3((unsigned)grid), dim3(kPagedThreads), smem, st, a);
     JOT_TRY(launch_check());
-    return a.whole ? JOT_OK : launch_join<T, HD>(a, grid, 16 * WM, st);
+    return a.whole ? JOT_OK : launch_join<T, HD>(a, grid, 16, st);
 }
 
 // (head_dim, key of the page, head, page); a box is 64 columns of a page's keys, or of 128 of them.  Out-of-range pages read as zeros.
@@ -200,7 +200,7 @@ template <typename T, int HD>
 int launch_paged(const DeviceInfo* di, const PagedArgs& a, int row_tile, cudaStream_t st) {
     const int rows = a.T * a.group;
     const int64_t items = (int64_t)a.nkv * ((rows + row_tile - 1) / row_tile);
-    if (row_tile == 16) return launch_paged_t<T, HD, 1>(di, a, items, st);
+    if (row_tile == 16) return launch_paged_t<T, HD>(di, a, items, st);
     if (row_tile == 32) return launch_paged_umma<T, HD, 32>(di, a, items, st);
     if (row_tile == 64) return launch_paged_umma<T, HD, 64>(di, a, items, st);
     return row_tile == 128 ? launch_paged_umma<T, HD, 128>(di, a, items, st) : launch_paged_umma<T, HD, 256>(di, a, items, st);

@@ -4,20 +4,25 @@
 //
 // key j of sequence b in page table[b, j / page_size] at offset j % page_size.  Bidirectional: no mask but the length.  The
 // rows of one key head (every new row of each of its query heads, row r = t * group + g) share its keys and are worked on
-// together, MT = 16, 32 or 64 at a time.
+// together: up to 16 of them here, on mma.sync, for a token of each sequence or a few; more in paged_attention_umma.cuh.
 //
 // Bound by HBM for few rows (the cache is read once: 2 * head_dim * 2 bytes a key, for R rows 4 R head_dim flops).  Sequences are
 // of any and unequal length, known on the device only, so the work is cut there: all tiles of 64 keys of all (sequence, key
-// head, row tile) items form one line, and CTA i of G takes the tiles [i W / G, (i + 1) W / G) of it, whatever items they belong
-// to.  An item that lies in one CTA's range is finished there; one that spans several leaves, per CTA, the unnormalised fp32
-// output with its maximum and sum, which a second kernel joins.  Where a table row has room for a few tiles only, items are not cut and
-// there is no second kernel.  Nothing is added with atomics: a call gives the same bits every time.
+// head, row tile) items form one line, and CTA i of G takes an equal share of it, whatever items that belongs to.  An item that lies in
+// one CTA's share is finished there; one that spans several leaves, per CTA, the unnormalised fp32 output with its maximum and sum,
+// which a second kernel joins.  Where a table row has room for a few tiles only, items are not cut and there is no second kernel.
+// Nothing is added with atomics: a call gives the same bits every time.
 //
-// A CTA keeps three stages of 64 keys in flight (cp.async, 16 bytes a request, a page table entry fetched one tile ahead); its four
-// warps share a stage as WM warps of 16 rows by 4 / WM ranges of keys, and each range keeps a maximum, a sum and an accumulator of
-// its own until the item ends.  16-byte chunk c of a row sits at position c ^ (row mod 8): eight rows of one chunk are on eight
-// different banks for ldmatrix.  Scores, statistics and accumulators are fp32; probabilities are rounded to the cache's type for
-// the second product (the sum is taken before the rounding).
+// A CTA keeps three stages of 64 keys in flight (cp.async, 16 bytes a request, a page table entry and the rows' addresses fetched
+// ahead), two CTAs an SM; its four warps have 16 keys of a stage each, and a maximum, a sum and an accumulator of their own until the
+// item ends.  16-byte chunk c of a row sits at position c ^ (row mod 8): eight rows of one chunk are on eight different banks for
+// ldmatrix.  Scores, statistics and accumulators are fp32; probabilities are rounded to the cache's type for the second product (the
+// sum is taken before the rounding).
+//
+// One row of 28 query over 4 key heads for four sequences of 40007 to 131072 keys (700 MB): 118-123 us, 5.7-6.0 TB/s, 0.87-0.91 of the copy;
+// what is left is the launch, the share's beginning and the second kernel (8 us together).  What it had been bound by: 920 instructions a
+// warp and tile, most of them addresses (140 us); now 16 loads of operands, 32 products, 32 requests.  On tcgen05, whose tile of 128
+// rows would be 7 / 128 full, the same 123 us, but a short call takes 2 us more, and pages that TMA cannot bring 168 us.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -228,10 +233,10 @@ struct PagedSmem {
     static constexpr int DYN_BYTES = kPagedStages * STAGE_BYTES + MERGE_BYTES;
 };
 
-template <typename T, int HD, int WM>
+template <typename T, int HD>
 __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const PagedArgs a) {
     using SM = PagedSmem<HD>;
-    constexpr int MT = 16 * WM, WK = 4 / WM, KW = kPagedTile / WK;      // rows; ranges of keys; keys of a range
+    constexpr int MT = 16, WK = 4, KW = kPagedTile / WK;                // rows; ranges of keys, a warp's each; keys of a range
     constexpr int NT = KW / 8, KS = HD / 16, DT = HD / 8;               // score tiles, steps of the first product, output tiles
     constexpr int CPR = HD / 8;                                         // 16-byte chunks of a key
     extern __shared__ __align__(128) uint8_t smem[];
@@ -324,7 +329,6 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     }
 
     // ---- products ----
-    const int wm = warp % WM, wk = warp / WM;
     const int g = lane >> 2, t4 = lane & 3;
     // operand addresses within a tile: a lane's row, and the swizzled position of chunk 2 i (+ 1) for i < 4; the next four lie 128 bytes on
     uint32_t kofs[4], vofs[4];
@@ -342,7 +346,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
         uint32_t qf[KS][4];
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
-            const int r = row0 + wm * 16 + g + 8 * hh, t = r / a.group, gq = r - t * a.group;
+            const int r = row0 + g + 8 * hh, t = r / a.group, gq = r - t * a.group;
             const T* qp = (const T*)a.q + b * a.q_b + (int64_t)t * a.q_t + (int64_t)(head * a.group + gq) * a.q_h;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -362,7 +366,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
             ++requested;
             leave_address(requested & 1);
             request_entry();
-            const uint32_t sk = s0 + stage * SM::STAGE_BYTES + wk * KW * (HD * 2), sv = sk + SM::TILE_BYTES;
+            const uint32_t sk = s0 + stage * SM::STAGE_BYTES + warp * KW * (HD * 2), sv = sk + SM::TILE_BYTES;
             if (++stage == kPagedStages) stage = 0;
             float s[NT][4];
 #pragma unroll
@@ -376,7 +380,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
                     MmaOp<T>::mma(s[j], qf[ks], kb[0], kb[1]);
                     MmaOp<T>::mma(s[j + 1], qf[ks], kb[2], kb[3]);
                 }
-            const int limit = n - kt * kPagedTile - wk * KW;            // keys of the range that exist
+            const int limit = n - kt * kPagedTile - warp * KW;            // keys of the range that exist
             float top[2] = {mx[0], mx[1]};
 #pragma unroll
             for (int j = 0; j < NT; ++j)
@@ -442,7 +446,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
         for (int hh = 0; hh < 2; ++hh) {
             sum[hh] += __shfl_xor_sync(0xffffffffu, sum[hh], 1);
             sum[hh] += __shfl_xor_sync(0xffffffffu, sum[hh], 2);
-            if (t4 == 0) ml[wk][wm * 16 + g + 8 * hh] = make_float2(mx[hh], sum[hh]);
+            if (t4 == 0) ml[warp][g + 8 * hh] = make_float2(mx[hh], sum[hh]);
         }
         __syncthreads();
         float mine[2];                                                  // what this warp's accumulators are multiplied by
@@ -450,7 +454,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
         for (int hh = 0; hh < 2; ++hh) {
             float m = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < WK; ++w) m = fmaxf(m, ml[w][wm * 16 + g + 8 * hh].x);
+            for (int w = 0; w < WK; ++w) m = fmaxf(m, ml[w][g + 8 * hh].x);
             mine[hh] = m == -INFINITY ? 1.f : ex2_approx(mx[hh] - m);
         }
         auto totals = [&](int r, float& m, float& l) {
@@ -478,7 +482,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
             for (int d = 0; d < QD; ++d)
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh)
-                    *reinterpret_cast<float2*>(merge + ((wk * MT + wm * 16 + g + 8 * hh) * QC + d * 8 + 2 * t4)) =
+                    *reinterpret_cast<float2*>(merge + ((warp * MT + g + 8 * hh) * QC + d * 8 + 2 * t4)) =
                         make_float2(o[quarter * QD + d][2 * hh] * mine[hh], o[quarter * QD + d][2 * hh + 1] * mine[hh]);
             __syncthreads();
             for (int i = tid; i < MT * (QC / 8); i += kPagedThreads) {

@@ -25,6 +25,13 @@
 //   by cp.async      warps 8-11 keys and values (ROWS <= 128: two a stream), warps 12, 13 products
 // The softmax warps bring the queries themselves, when a part begins: their room is the one that the previous part has left through.
 //
+// 32 rows of 32 heads of 16 sequences of 384 to 704 keys (143 MB): 44.9 us, 3.4 TB/s; bound by the chain a short item is (queries, first
+// scores, exponentials, second product, way out: 15 us for its four tiles), which two streams hide half of.  Before: 59.5 us on
+// mma.sync in tiles of 32 rows, 66 as one stream of even and odd tiles, which ended its items together.
+// 224 rows a key head of eight sequences of 2001 to 9001 keys (20 GFLOP): 53 us, 380 TFLOP/s; bound by a tile's chain (exponentials 2.4k
+// cycles, of which a quarter waits for stores to tensor memory, and the two products 1.9k) and by the parts' ends; 104 us on mma.sync.  256
+// rows of 704 over 704 keys: 557 TFLOP/s.
+//
 // Every barrier is waited on phase by phase by whoever waits on it, so that a parity says which phase is meant.  All waits end: one
 // that gives up makes the CTA leave, after its copies and products under way have ended.
 #pragma once

@@ -6,6 +6,7 @@ fallback: if the library is missing or fails to load, importing the binding's fu
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import dataclasses
 import functools
@@ -680,8 +681,10 @@ def kv_copy_pages(pages: KVPages, src: Sequence[int], dst: Sequence[int]) -> Non
     if len(src) != len(dst):
         raise ValueError("kv_copy_pages: src and dst differ in length")
     n = len(src)
+    src, dst = array.array("i", src), array.array("i", dst)      # refuses what is no 32-bit integer
     pair = C.c_int32 * n
-    _launch(pages.device, "jot_kv_copy_pages", _lib().jot_kv_copy_pages, pages._ref, n, pair(*src), pair(*dst))
+    _launch(pages.device, "jot_kv_copy_pages", _lib().jot_kv_copy_pages, pages._ref, n, pair.from_buffer(src) if n else None,
+            pair.from_buffer(dst) if n else None)
 
 
 @functools.lru_cache(maxsize=None)

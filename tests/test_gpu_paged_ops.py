@@ -484,6 +484,9 @@ def test_refusals_on_the_device(jot):
     refused(-1, lambda: jot.kv_write(pages, x[:, :2], x[:, 2:], rows, layer=-1))
     for src, dst in (([0], [pages.n_pages]), ([-1], [0]), ([0, 1], [2, 2]), ([0, 1], [1, 2]), ([0], [0])):
         refused(-1, lambda: jot.kv_copy_pages(pages, src, dst))
+    for pages_bad in ([2 ** 32], [-2 ** 31 - 1]):
+        with pytest.raises(OverflowError):
+            jot.kv_copy_pages(pages, pages_bad, [1])
     assert jot.launch_count() == n0
     for bad in (lambda: jot.paged_attention(q.half(), pages, table, lens), lambda: jot.paged_attention(q, pages, table.long(), lens),
                 lambda: jot.paged_attention(q, pages, table, lens.cpu()), lambda: jot.head_norm_rope(x.float(), None, rows, jot.Rope(jot.rope_frequencies(64, 1e4))),
