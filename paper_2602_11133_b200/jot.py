@@ -12,6 +12,7 @@ import dataclasses
 import functools
 import math
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import torch
@@ -88,19 +89,11 @@ class _Trace(C.Structure):
                 ("n_candidates", C.c_void_p)]
 
 
-class _KVPages(C.Structure):
-    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_layer_stride", C.c_int64), ("v_layer_stride", C.c_int64),
-                ("k_page_stride", C.c_int64), ("v_page_stride", C.c_int64), ("n_layers", C.c_int32), ("n_pages", C.c_int32),
-                ("n_kv_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
-
-
-class _Rope(C.Structure):
-    _fields_ = [("inv_freq", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float)]
-
-
-class _Heads(C.Structure):
-    _fields_ = [("src", C.c_void_p), ("in_row_stride", C.c_int64), ("in_head_stride", C.c_int64), ("out", C.c_void_p),
-                ("out_row_stride", C.c_int64), ("out_head_stride", C.c_int64), ("gain", C.c_void_p), ("n_heads", C.c_int32)]
+# The small structs of the paged calls as packed bytes (native sizes and alignment): a ctypes.Structure takes a microsecond to fill, three or
+# four of them a third of a short call.
+_pack_pages = struct.Struct("PPqqqqiiiiii").pack     # jot_kv_pages: k, v, strides of layers (k, v) and pages (k, v), layers, pages, heads, page size, head_dim, dtype
+_pack_rope = struct.Struct("Piif4x").pack            # jot_rope: inv_freq, rotary_dim, interleaved, magnitude
+_pack_heads = struct.Struct("PqqPqqPi4x").pack       # jot_heads: in, strides (row, head), out, strides, gain, n_heads
 
 
 @dataclasses.dataclass
@@ -162,8 +155,8 @@ def _lib():
         lib.jot_read_status.argtypes = [C.c_void_p, C.c_void_p]
         lib.jot_profile.argtypes = [C.c_void_p, C.c_int]
         lib.jot_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.c_int]
-        heads, pages = C.POINTER(_Heads), C.POINTER(_KVPages)
-        lib.jot_head_norm_rope.argtypes = [heads, heads, C.POINTER(_Rope), C.c_int, C.c_int, C.c_int, C.c_float, C.c_void_p,
+        heads = rope = pages = C.c_void_p        # structs, or bytes packed as they are
+        lib.jot_head_norm_rope.argtypes = [heads, heads, rope, C.c_int, C.c_int, C.c_int, C.c_float, C.c_void_p,
                                            heads, pages, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
         lib.jot_kv_write.argtypes = [pages, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64,
                                      C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
@@ -300,7 +293,7 @@ class Model:
             raise ValueError(f"attach_kv_pages: the table has {page_table.shape[0]} rows, the model takes {self.max_batch} sequences")
         nbytes = _lib().jot_kv_pages_workspace_bytes(C.byref(self.cfg), self.max_batch, self.max_seq)
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        _check(_lib().jot_attach_kv_pages(self.handle, pages._ref, page_table.data_ptr(), page_table.stride(0), page_table.shape[1],
+        _check(_lib().jot_attach_kv_pages(self.handle, pages._packed, page_table.data_ptr(), page_table.stride(0), page_table.shape[1],
                                           workspace.data_ptr(), nbytes), "jot_attach_kv_pages")
         self.kv_cache = (pages, page_table, workspace)       # keep them alive
 
@@ -556,7 +549,7 @@ class KVPages:
     (its last three dimensions) is contiguous; layers and pages may lie at any stride that is a multiple of 8 elements, so
     that k and v may be two halves of one tensor.  The tensors are borrowed and written in place."""
 
-    __slots__ = ("k", "v", "device", "dtype", "n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim", "_c", "_ref")
+    __slots__ = ("k", "v", "device", "dtype", "n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim", "_packed")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         shape, ks, vs, device, dtype = k.shape, k.stride(), v.stride(), k.device, k.dtype
@@ -570,9 +563,8 @@ class KVPages:
                 raise TypeError("KVPages: the last three dimensions must be contiguous")
         self.k, self.v, self.device, self.dtype = k, v, device, dtype
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
-        self._c = _KVPages(k.data_ptr(), v.data_ptr(), ks[0], vs[0], ks[1], vs[1], n_layers, n_pages, n_kv_heads, page_size, head_dim,
-                           _ELEMENTS[dtype])
-        self._ref = C.byref(self._c)
+        self._packed = _pack_pages(k.data_ptr(), v.data_ptr(), ks[0], vs[0], ks[1], vs[1], n_layers, n_pages, n_kv_heads, page_size, head_dim,
+                                   _ELEMENTS[dtype])
 
     @staticmethod
     def empty(n_layers: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype=torch.bfloat16,
@@ -610,15 +602,15 @@ def rope_frequencies(rotary_dim: int, theta: float, factor: float = 1.0, origina
 
 
 def _heads(x: torch.Tensor, out: Optional[torch.Tensor], gain: Optional[torch.Tensor], name: str, device, dtype, rows: int, hd: int,
-           fresh: bool = False) -> _Heads:
-    """fresh: out was made here, like x."""
+           fresh: bool = False) -> bytes:
+    """A packed jot_heads.  fresh: out was made here, like x."""
     n = x.shape[1]
     shape = (rows, n, hd)
     xs = _element_strides(x, name, dtype, device, shape)
     outs = (0, 0) if out is None else out.stride() if fresh else _element_strides(out, name + "_out", dtype, device, shape)
     if gain is not None and (gain.dtype != dtype or gain.device != device or gain.dim() != 1 or gain.numel() != hd or not gain.is_contiguous()):
         raise TypeError(f"{name}_gain: expected a contiguous {dtype} tensor [{hd}] on {device}")
-    return _Heads(x.data_ptr(), xs[0], xs[1], None if out is None else out.data_ptr(), outs[0], outs[1], None if gain is None else gain.data_ptr(), n)
+    return _pack_heads(x.data_ptr(), xs[0], xs[1], 0 if out is None else out.data_ptr(), outs[0], outs[1], 0 if gain is None else gain.data_ptr(), n)
 
 
 def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, rope: Rope,
@@ -649,17 +641,17 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.
         if k is not None:
             if k_out is None:
                 k_out = torch.empty_like(k)
-            hk = C.byref(_heads(k, k_out, k_gain, "k", device, dtype, rows, hd, fresh_k))
+            hk = _heads(k, k_out, k_gain, "k", device, dtype, rows, hd, fresh_k)
     else:
         if k is None or v is None or slots is None or k_out is not None:
             raise ValueError("head_norm_rope: pages need k, v and slots, and take the place of k_out")
         if pages.device != device:
             raise TypeError(f"pages: expected on {device}, got {pages.device}")
-        ref = pages._ref
-        hk = C.byref(_heads(k, None, k_gain, "k", device, dtype, rows, hd))
-        hv = C.byref(_heads(v, None, None, "v", device, dtype, rows, hd))
-    _launch(device, "jot_head_norm_rope", _lib().jot_head_norm_rope, C.byref(_heads(q, q_out, q_gain, "q", device, dtype, rows, hd, fresh_q)), hk,
-            C.byref(_Rope(f.data_ptr(), 2 * f.numel(), rope.interleaved, rope.magnitude)), _ELEMENTS[dtype], rows, hd, eps,
+        ref = pages._packed
+        hk = _heads(k, None, k_gain, "k", device, dtype, rows, hd)
+        hv = _heads(v, None, None, "v", device, dtype, rows, hd)
+    _launch(device, "jot_head_norm_rope", _lib().jot_head_norm_rope, _heads(q, q_out, q_gain, "q", device, dtype, rows, hd, fresh_q), hk,
+            _pack_rope(f.data_ptr(), 2 * f.numel(), rope.interleaved, rope.magnitude), _ELEMENTS[dtype], rows, hd, eps,
             _int_ptr(positions, "positions", device, rows), hv, ref, layer, _int_ptr(slots, "slots", device, rows),
             _int_ptr(status, "status", device, 1))
     return q_out, k_out
@@ -672,7 +664,7 @@ def kv_write(pages: KVPages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tens
     device, rows = pages.device, k.shape[0]
     shape = (rows, pages.n_kv_heads, pages.head_dim)
     ks, vs = _element_strides(k, "k", pages.dtype, device, shape), _element_strides(v, "v", pages.dtype, device, shape)
-    _launch(device, "jot_kv_write", _lib().jot_kv_write, pages._ref, layer, rows, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+    _launch(device, "jot_kv_write", _lib().jot_kv_write, pages._packed, layer, rows, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
             _int_ptr(slots, "slots", device, rows), _int_ptr(status, "status", device, 1))
 
 
@@ -683,7 +675,7 @@ def kv_copy_pages(pages: KVPages, src: Sequence[int], dst: Sequence[int]) -> Non
     n = len(src)
     src, dst = array.array("i", src), array.array("i", dst)      # refuses what is no 32-bit integer
     pair = C.c_int32 * n
-    _launch(pages.device, "jot_kv_copy_pages", _lib().jot_kv_copy_pages, pages._ref, n, pair.from_buffer(src) if n else None,
+    _launch(pages.device, "jot_kv_copy_pages", _lib().jot_kv_copy_pages, pages._packed, n, pair.from_buffer(src) if n else None,
             pair.from_buffer(dst) if n else None)
 
 
@@ -723,7 +715,7 @@ def paged_attention(q: torch.Tensor, pages: KVPages, page_table: torch.Tensor, l
     elif workspace.dtype != torch.uint8 or workspace.device != device or not workspace.is_contiguous():
         raise TypeError(f"workspace: expected a contiguous uint8 tensor on {device}")
     _launch(device, "jot_paged_attention", _lib().jot_paged_attention, q.data_ptr(), qs[0], qs[1], qs[2], out.data_ptr(), outs[0], outs[1], outs[2],
-            None if lse is None else lse.data_ptr(), B, T, nq, pages._ref, layer, page_table.data_ptr(), page_table.stride(0), table[1],
+            None if lse is None else lse.data_ptr(), B, T, nq, pages._packed, layer, page_table.data_ptr(), page_table.stride(0), table[1],
             _int_ptr(lens, "lens", device, B), hd ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel(),
             _int_ptr(status, "status", device, 1))
     return out

@@ -26,7 +26,8 @@ def pages_struct(jot, **kw):
     d = dict(k=PTR, v=PTR, k_layer_stride=0, v_layer_stride=0, k_page_stride=4 * 16 * 64, v_page_stride=4 * 16 * 64, n_layers=1, n_pages=8, n_kv_heads=4,
              page_size=16, head_dim=64, dtype=0)
     d.update(kw)
-    return jot._KVPages(**d)
+    order = ("k", "v", "k_layer_stride", "v_layer_stride", "k_page_stride", "v_page_stride", "n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim", "dtype")
+    return jot._pack_pages(*(d[x] or 0 for x in order))
 
 
 BAD_PAGES = [(dict(k=None), ARG), (dict(v=PTR + 8), ARG), (dict(n_pages=0), ARG), (dict(page_size=-1), ARG), (dict(dtype=2), ARG), (dict(head_dim=60), SHAPE),
@@ -52,8 +53,8 @@ def test_layers_out_of_range_are_refused(jot):
 
 def test_head_norm_rope_refusals(jot):
     lib = jot._lib()
-    H = lambda n=4, src=PTR, out=PTR, row=256, head=64, gain=None: jot._Heads(src, row, head, out, row, head, gain, n)
-    rope = lambda rotary=64, il=0, freq=PTR: jot._Rope(freq, rotary, il, 1.0)
+    H = lambda n=4, src=PTR, out=PTR, row=256, head=64, gain=None: jot._pack_heads(src, row, head, out or 0, row, head, gain or 0, n)
+    rope = lambda rotary=64, il=0, freq=PTR: jot._pack_rope(freq or 0, rotary, il, 1.0)
 
     def call(q=None, k=None, r=None, dtype=0, rows=2, hd=64, pos=PTR, v=None, pages=None, layer=0, slots=None):
         return lib.jot_head_norm_rope(q or H(), k, r or rope(), dtype, rows, hd, 1e-6, pos, v, pages, layer, slots, None, None)
