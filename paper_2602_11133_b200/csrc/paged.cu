@@ -99,12 +99,17 @@ PagedSpace paged_space(int row_tile, int head_dim) {
     return s;
 }
 
+// Items of a call: (sequence, key head, tile of rows).
+int64_t paged_items(const PagedArgs& a, int row_tile) { return (int64_t)a.B * a.nkv * ((a.T * a.group + row_tile - 1) / row_tile); }
+
 // The second kernel: four warps to a row where an item may be in many parts (few items on many CTAs), else a warp to a row.
 template <typename T, int HD>
-int launch_join(const PagedArgs& a, int grid, int row_tile, cudaStream_t st) {
-    const int all = a.T * a.group, rows = std::min(row_tile, all), row_tiles = (all + row_tile - 1) / row_tile;
+int launch_join(const PagedArgs& a, int shares, int row_tile, cudaStream_t st) {
+    const int rows = std::min(row_tile, a.T * a.group);
+    const int64_t items = paged_items(a, row_tile);
+    const int grid = a.by_item ? (int)items : shares;
     auto go = [&](auto* kernel, int per_cta) { launch_k(kernel, dim3((unsigned)grid, (unsigned)((rows + per_cta - 1) / per_cta)), dim3(kPagedThreads), 0, st, a, row_tile); };
-    if (grid > 8ll * a.B * a.nkv * row_tiles) go(paged_join_kernel<T, HD, 4>, 1);
+    if (shares > 8 * items) go(paged_join_kernel<T, HD, 4>, 1);
     else go(paged_join_kernel<T, HD, 1>, 4);
     return launch_check();
 }
@@ -137,6 +142,7 @@ int launch_paged_t(const DeviceInfo* di, PagedArgs a, int64_t items, cudaStream_
     const int64_t tiles = paged_tiles(a, kPagedTile);
     a.whole = tiles <= kPagedWhole;
     const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(occ * di->sms, kPagedMaxCtas));
+    a.by_item = !a.whole && paged_items(a, 16) <= grid;
     launch_k(kernel, dim3((unsigned)grid), dim3(kPagedThreads), smem, st, a);
     JOT_TRY(launch_check());
     return a.whole ? JOT_OK : launch_join<T, HD>(a, grid, 16, st);
@@ -191,6 +197,7 @@ int launch_paged_umma(const DeviceInfo* di, PagedArgs a, int64_t items, cudaStre
     // two tiles of rows take twice as long over a tile of keys: worth cutting unless a third of the SMs have items of their own
     a.whole = tiles <= 1 || (tiles <= kPagedWhole && (ROWS < 256 || 3 * items * a.B >= di->sms));
     const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(di->sms, kUmmaPagedMaxCtas));
+    a.by_item = !a.whole && paged_items(a, ROWS) <= grid * streams;
     if (tma) JOT_TRY((launch_paged_umma_t<T, HD, ROWS, true>(di, a, grid, st)));
     else JOT_TRY((launch_paged_umma_t<T, HD, ROWS, false>(di, a, grid, st)));
     return a.whole ? JOT_OK : launch_join<T, HD>(a, grid * streams, ROWS, st);

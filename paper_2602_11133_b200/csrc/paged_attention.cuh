@@ -53,7 +53,8 @@ struct PagedArgs {
     float scale_log2;                       // scale * log2(e)
     bool whole;                             // items are not cut: shares are whole items, and nothing is left to join
     // workspace: one descriptor per CTA, then two partial results per CTA
-    int4* desc;                             // (sequence, item within it, fragments, -) of the item that begins in CTA i and ends in a later one
+    int4* desc;                             // (sequence, item within it, parts, share it begins in); parts 0: not cut
+    bool by_item;                           // one per item (there are at most as many as shares), else one per share: the item that begins there
     float* partial;                         // [CTA][2][MT][HD] unnormalised outputs
     float2* partial_ml;                     // [CTA][2][MT] (maximum in base 2, sum)
     int32_t* status;
@@ -225,6 +226,13 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
     return rg;
 }
 
+// What the second kernel has to know of an item that begins in `share`, whose last `behind` tiles lie behind the share's end.
+__device__ __forceinline__ void paged_describe(const PagedArgs& a, const PagedRange& rg, int share, int per_b, int b, int item, int behind) {
+    const int parts = behind > 0 ? paged_owner(rg.total, rg.ctas, rg.end + behind - 1) - share + 1 : 0;
+    if (a.by_item) a.desc[b * per_b + item] = make_int4(b, item, parts, share);
+    else if (parts > 0) a.desc[share] = make_int4(b, item, parts, share);
+}
+
 template <int HD>
 struct PagedSmem {
     static constexpr int TILE_BYTES = kPagedTile * HD * 2;                       // K or V of one stage
@@ -252,7 +260,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     const int per_b = a.nkv * RT;                                       // items of a sequence
 
     const PagedRange rg = paged_range<T, HD, kPagedThreads, 1>(a, kPagedTile, per_b, 0, range_smem);
-    if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (tid == 0 && !a.by_item) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if ((int)blockIdx.x >= rg.ctas) return;
 
     // ---- loads: a walk over the tiles of the share ----
@@ -511,11 +519,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
             }
             __syncthreads();
         }
-        if (begins && !ends && tid == 0) {
-            // tiles of the line from the item's first to its last; the next CTAs have the rest of them
-            const int last = rg.end + (nt - kt_end) - 1;
-            a.desc[blockIdx.x] = make_int4(b, item, paged_owner(rg.total, rg.ctas, last) - (int)blockIdx.x + 1, 0);
-        }
+        if (begins && tid == 0) paged_describe(a, rg, blockIdx.x, per_b, b, item, nt - kt_end);
         // next item
         kt = 0;
         if (++item == per_b && left > 0) {
@@ -527,8 +531,8 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
     cp_async_wait<0>();
 }
 
-// Joins the parts of the items that several CTAs worked on.  blockIdx.x: the CTA in which an item begins; WPR warps share a row, a part
-// of the parts each, a lane HD / 32 columns.
+// Joins the parts of the items that several CTAs worked on.  blockIdx.x: the descriptor; WPR warps share a row, a part of the parts each, a
+// lane HD / 32 columns.
 template <typename T, int HD, int WPR>
 __global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedArgs a, int MT) {
     grid_launch_dependents();
@@ -536,16 +540,18 @@ __global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedAr
     constexpr int E = HD / 32;
     __shared__ float so[WPR > 1 ? 4 : 1][HD];
     __shared__ float2 sml[4];
+    const int R = a.T * a.group, RT = (R + MT - 1) / MT;
+    if (a.by_item && paged_len(a, blockIdx.x / (a.nkv * RT)) <= 0) return;      // nobody had this item
     const int4 d = a.desc[blockIdx.x];
     if (d.z == 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int R = a.T * a.group, RT = (R + MT - 1) / MT, head = d.y / RT, row0 = (d.y - head * RT) * MT;
+    const int head = d.y / RT, row0 = (d.y - head * RT) * MT;
     const int r = blockIdx.y * (4 / WPR) + warp / WPR;
     if (r >= min(MT, R - row0)) return;                                 // (with WPR = 4 all of the CTA's warps have this row)
     float m = -INFINITY, l = 0.f, o[E] = {};
 #pragma unroll 4
     for (int f = warp % WPR; f < d.z; f += WPR) {
-        const int64_t at = (f == 0 ? (int64_t)blockIdx.x * 2 + 1 : (int64_t)(blockIdx.x + f) * 2) * MT + r;
+        const int64_t at = (f == 0 ? (int64_t)d.w * 2 + 1 : (int64_t)(d.w + f) * 2) * MT + r;
         const float2 p = a.partial_ml[at];
         float x[E];
 #pragma unroll

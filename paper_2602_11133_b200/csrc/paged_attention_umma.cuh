@@ -188,7 +188,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     const int s = warp < 8 ? warp >> 2 : (warp >= Role::MMA ? warp - Role::MMA : (TWO ? 0 : (warp - Role::PROD) / Role::PROD_WARPS));
     const PagedRange rg = paged_range<T, HD, THREADS, STREAMS>(a, KEYS, per_b, TWO ? 0 : s, range_smem);
     const int share = (TWO ? 0 : s) * gridDim.x + blockIdx.x;      // first one for every CTA, then a second
-    if (tid < STREAMS) a.desc[tid * gridDim.x + blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (tid < STREAMS && !a.by_item) a.desc[tid * gridDim.x + blockIdx.x] = make_int4(0, 0, 0, 0);
     __syncthreads();                             // (a descriptor is written again below)
     auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {
         const bool w = mbar_wait(bar, parity, abortp);
@@ -678,10 +678,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 if (!whole) a.partial_ml[slot * ROWS + base0 + r128] = make_float2(m, sum);
                 else if (a.lse) a.lse[((int64_t)w.b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(sum)) * 0.69314718055994531f;
             }
-            if (begins && !whole && (tid & 127) == 0 && (!TWO || s == 0)) {
-                const int last = rg.end + (w.nt - w.cnt) - 1;      // the item's last tile on the line: the next shares have the rest of it
-                a.desc[share] = make_int4(w.b, w.item, paged_owner(rg.total, rg.ctas, last) - share + 1, 0);
-            }
+            if (begins && (tid & 127) == 0 && (!TWO || s == 0)) paged_describe(a, rg, share, per_b, w.b, w.item, w.nt - w.cnt);
             more = w.next(a, per_b, KEYS);
         }
     }
