@@ -13,6 +13,8 @@
 //                 few rows wait for, is a half or a quarter.  The copies are added up at the end.
 //   ROWS = 256    the streams are two tiles of 128 rows over the same keys, and take turns in their exponentials: at the same time, they
 //                 would only get half of the special function units each, and then both wait for the tensor pipe.
+// Where a thread has a whole row (128 or 256 rows) a stream has two score buffers of 64 keys, and the scores of one are made while the
+// probabilities of the other are: a thread's chain is its exponentials alone.
 // The reference maximum of a row follows a tile's maximum only when that exceeds it by more than 2^8 (probabilities up to 256
 // are as exact as those up to 1); then the row of the accumulator is rescaled in tensor memory.
 //
@@ -119,7 +121,8 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     constexpr int KB = HD / 64, ST = SM::STAGES, RING = TWO ? ST : ST / 2, TILE = kUmmaPagedTile, THREADS = Role::THREADS;
     constexpr int STREAMS = TWO ? 1 : 2;                          // shares of the line a CTA has
     constexpr int REP = TWO ? 1 : 128 / ROWS, KC = 128 / REP;     // copies of a row, and keys of a tile that one takes
-    constexpr uint32_t IDESC_S = umma_idesc16<T>(128, 128, false), IDESC_O = umma_idesc16<T>(128, HD, true);
+    constexpr int HV = KC == 128 ? 2 : 1, HK = 128 / HV;          // score buffers of a stream, and keys of one
+    constexpr uint32_t IDESC_S = umma_idesc16<T>(128, HK, false), IDESC_O = umma_idesc16<T>(128, HD, true);
     constexpr uint32_t O_COL = 256;              // scores of the streams at columns 0 and 128, accumulators at 256 and 384
     constexpr float kRaise = 8.f;
 
@@ -127,7 +130,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * SM::TILE_BYTES, sV = sK + ST * SM::TILE_BYTES;
     uint8_t* const values_at = smem + (2 + ST) * SM::TILE_BYTES;
-    __shared__ uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], q_full[2], s_full[2], p_full[2], pv_done[2], o_empty[2],
+    __shared__ uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], q_full[2], s_full[2][HV], p_full[2][HV], pv_done[2][HV], o_empty[2],
         drain[2], turn[2], tail_bar, prod_bar[2], g_bar[2];
     __shared__ uint64_t row_at[TMA ? 1 : STREAMS][2][TMA ? 1 : 2 * TILE];      // by cp.async: addresses of a tile's key rows, then of its value rows; odd: no such row
     __shared__ uint64_t row_q[2][128], row_o[2][2][128];     // addresses of the rows' queries, and of their results ([parity of the part])
@@ -147,9 +150,11 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 128);                                      // every softmax thread's requests
-            mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i], 4);
-            mbar_init(&pv_done[i], 1);
+            for (int h = 0; h < HV; ++h) {
+                mbar_init(&s_full[i][h], 1);
+                mbar_init(&p_full[i][h], 4);
+                mbar_init(&pv_done[i][h], 1);
+            }
             mbar_init(&o_empty[i], 4);
             mbar_init(&drain[i], 1);
             mbar_init(&turn[i], 4);
@@ -356,77 +361,87 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         const uint64_t qd = umma_desc_k128(sQ + s * SM::TILE_BYTES), kd0 = umma_desc_k128(sK), vd0 = umma_desc_mn128(sV);
         const uint32_t d_s = tmem_base + s * 128, d_o = tmem_base + O_COL + s * 128;
         PagedWalk w(rg, KEYS);
-        uint32_t part = 0, made = 0, done = 0, tails = 0;          // parts, first and second products, tails so far
+        uint32_t part = 0, base = 0, tails = 0, done[HV] = {};     // parts, tiles, tails so far; second products per buffer
         bool ok = true, more = true;
         for (; ok && more; ++part) {
             const int tail = w.n - (w.nt - 1) * KEYS;              // keys of the last tile of the sequence
-            const bool has_tail = TMA && w.kt + w.cnt == w.nt && tail < KEYS;
+            const bool ends = w.kt + w.cnt == w.nt, has_tail = TMA && ends && tail < KEYS;
+            const int units = w.cnt * HV - (ends && tail <= (HV - 1) * HK);       // buffers' worth of keys: the last one may hold none
+            auto stage = [&](int u) -> uint32_t { return (TWO ? 0 : s * RING) + (base + u / HV) % RING; };
+            auto phase = [&](int u) -> uint32_t { return (base + u / HV) / RING & 1; };
             ok = wait_all(&q_full[s], part & 1);
             if (ok) fence_proxy_async_smem();                      // the queries are written as threads write; the tensor pipe reads as copies do
-            auto issue_S = [&]() -> bool {
-                const uint32_t st = (TWO ? 0 : s * RING) + made % RING;
-                if (!wait_all(&k_full[st], made / RING & 1)) return false;
-                // the score buffer holds the probabilities of the stream's previous tile until its second product is done
-                if (done > 0 && !wait_all(&pv_done[s], (done - 1) & 1)) return false;
+            auto issue_S = [&](int u) -> bool {
+                const int h = u % HV;
+                const uint32_t st = stage(u);
+                if (h == 0 && !wait_all(&k_full[st], phase(u))) return false;
+                // the score buffer holds the probabilities of its previous keys until their second product is done
+                if (done[h] > 0 && !wait_all(&pv_done[s][h], (done[h] - 1) & 1)) return false;
                 if (!TMA) fence_proxy_async_smem();
                 tc_fence_after();
                 if (elected) {
-                    const uint64_t kd = kd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
+                    const uint64_t kd = kd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4) + h * (HK * 8));
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) umma_bf16(d_s, qd + kb * 1024 + 2 * k, kd + kb * 1024 + 2 * k, IDESC_S, (kb | k) != 0);
-                    umma_commit(&s_full[s]);
-                    umma_commit(&k_empty[st]);
+                        for (int k = 0; k < 4; ++k) umma_bf16(d_s + h * HK, qd + kb * 1024 + 2 * k, kd + kb * 1024 + 2 * k, IDESC_S, (kb | k) != 0);
+                    umma_commit(&s_full[s][h]);
+                    if (h == HV - 1 || u == units - 1) umma_commit(&k_empty[st]);
                 }
                 __syncwarp();
-                ++made;
                 return true;
             };
             auto issue_PV = [&](int u) -> bool {
-                const uint32_t st = (TWO ? 0 : s * RING) + done % RING;
-                if (!wait_all(&v_full[st], done / RING & 1)) return false;
-                if (has_tail && u == w.cnt - 1) {
-                    // value rows behind the sequence's end, whatever the page holds there, and those of boxes that were not fetched
-                    if (!TWO || s == 0) {
-                        for (int kb = 0; kb < KB; ++kb)
-                            for (int i = lane; i < (KEYS - tail) * 8; i += 32)
-                                reinterpret_cast<uint4*>(values_at + st * SM::TILE_BYTES + kb * 16384 + tail * 128)[i] = make_uint4(0, 0, 0, 0);
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                    }
-                    if (TWO) {                                     // the streams' warps meet: both see the zeros, and neither is a tail ahead
-                        if (lane == 0) mbar_arrive(&tail_bar);
-                        if (!wait_all(&tail_bar, tails & 1)) return false;
+                const int h = u % HV;
+                const uint32_t st = stage(u);
+                if (h == 0) {
+                    if (!wait_all(&v_full[st], phase(u))) return false;
+                    if (has_tail && u / HV == w.cnt - 1) {
+                        // value rows behind the sequence's end, whatever the page holds there, and those of boxes that were not fetched
+                        if (!TWO || s == 0) {
+                            for (int kb = 0; kb < KB; ++kb)
+                                for (int i = lane; i < (KEYS - tail) * 8; i += 32)
+                                    reinterpret_cast<uint4*>(values_at + st * SM::TILE_BYTES + kb * 16384 + tail * 128)[i] = make_uint4(0, 0, 0, 0);
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                        }
+                        if (TWO) {                                 // the streams' warps meet: both see the zeros, and neither is a tail ahead
+                            if (lane == 0) mbar_arrive(&tail_bar);
+                            if (!wait_all(&tail_bar, tails & 1)) return false;
+                        }
                     }
                 }
-                if (!wait_all(&p_full[s], done & 1)) return false;
+                if (!wait_all(&p_full[s][h], done[h] & 1)) return false;
                 if (!TMA) fence_proxy_async_smem();
                 tc_fence_after();
                 if (elected) {
                     const uint64_t vd = vd0 + (uint64_t)(st * (SM::TILE_BYTES >> 4));
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) umma_bf16_ts(d_o, d_s + (k < 4 ? 8 * k : 64 + 8 * (k - 4)), vd + k * 128, IDESC_O, u > 0 || k > 0);
-                    umma_commit(&pv_done[s]);
-                    umma_commit(&v_empty[st]);
+                    for (int k = 0; k < 8 / HV; ++k) {             // 16 keys: 8 columns of probabilities (64 keys in 32 columns from 0 and from 64 on), 16 value rows
+                        const int kk = h * (8 / HV) + k;
+                        umma_bf16_ts(d_o, d_s + kk / 4 * 64 + kk % 4 * 8, vd + kk * 128, IDESC_O, u > 0 || k > 0);
+                    }
+                    umma_commit(&pv_done[s][h]);
+                    if (h == HV - 1 || u == units - 1) umma_commit(&v_empty[st]);
                 }
                 __syncwarp();
-                ++done;
+                ++done[h];
                 return true;
             };
-            if (ok) ok = issue_S();
+            for (int u = 0; ok && u < min(HV, units); ++u) ok = issue_S(u);
             // the part's first products overwrite the accumulator: the previous part's rows must have left
             if (ok && part > 0) ok = wait_all(&o_empty[s], (part - 1) & 1);
-            for (int u = 0; ok && u < w.cnt; ++u) {
+            for (int u = 0; ok && u < units; ++u) {
                 ok = issue_PV(u);
-                if (ok && u + 1 < w.cnt) ok = issue_S();
+                if (ok && u + HV < units) ok = issue_S(u + HV);
             }
             tails += has_tail;
+            base += w.cnt;
             if (ok) more = w.next(a, per_b, KEYS);
         }
         // the last arrival the tensor pipe owes this CTA's barriers; where somebody gave up, the end of the products under way
         if (ok) {
-            wait_all(&v_empty[(TWO ? 0 : s * RING) + (done - 1) % RING], (done - 1) / RING & 1);
+            wait_all(&v_empty[(TWO ? 0 : s * RING) + (base - 1) % RING], (base - 1) / RING & 1);
         } else {
             if (elected) umma_commit(&drain[s]);
             __syncwarp();
@@ -440,7 +455,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         const float c = a.scale_log2, none = c < 0.f ? INFINITY : -INFINITY;
         float* const room = reinterpret_cast<float*>(smem + s * SM::TILE_BYTES);
         PagedWalk w(rg, KEYS);
-        uint32_t done = 0, part = 0, g_ph = 0;                     // tiles, parts so far
+        uint32_t done = 0, seen[HV] = {}, part = 0, g_ph = 0;      // buffers' worth of keys so far, and of each buffer; parts
         bool ok = true, more = true;
         auto group_sync = [&]() -> bool {                          // of the stream's four warps
             __syncwarp();
@@ -472,63 +487,43 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 cp_async_arrive(&q_full[s]);
             }
             float mc = -INFINITY, l = 0.f;
-            for (int i = 0; i < w.cnt; ++i, ++done) {
-                if (!(ok = wait_all(&s_full[s], done & 1))) break;
+            const int tail = w.n - (w.nt - 1) * KEYS, units = w.cnt * HV - (w.kt + w.cnt == w.nt && tail <= (HV - 1) * HK);
+            for (int u = 0; u < units; ++u, ++done) {
+                const int h = u % HV;
+                const uint32_t sb = sc + h * HK;                   // this buffer
+                if (!(ok = wait_all(&s_full[s][h], seen[h] & 1))) break;
+                ++seen[h];
                 if (!idle) {
                     tc_fence_after();
-                    // keys of the tile that exist, from the first one of this copy on
-                    const int limit = min(w.n - (w.kt + i) * KEYS, KEYS) - rep * KC;
-                    constexpr bool WIDE = TMA && KC == 128;        // room for all of a row's scores in registers
-                    float v[64], v2[WIDE ? 64 : 1], bm = none;
-                    auto maximum = [&](float* x, int first, int count) {
-                        if (limit < first + count) {
+                    // keys of the buffer that exist, from the first one of this copy on
+                    const int limit = min(w.n - (w.kt + u / HV) * KEYS, KEYS) - h * HK - rep * KC;
+                    constexpr int MINE = KC / HV;                  // keys of this thread
+                    float v[MINE], bm = none;
 #pragma unroll
-                            for (int t = 0; t < count; ++t)
-                                if (first + t >= limit) x[t] = none;
-                        }
-                        if (c < 0.f) {
+                    for (int t = 0; t < MINE; t += 32) tmem_ld32(sb + rep * KC + t, v + t);
 #pragma unroll
-                            for (int t = 0; t < count; ++t) bm = fminf(bm, x[t]);
-                        } else {
-                            float b1 = none;
+                    for (int t = 0; t < MINE; t += 32) tmem_ld_wait_regs(v + t);
+                    if (limit < MINE) {
 #pragma unroll
-                            for (int t = 0; t < count; t += 4) {
-                                bm = fmaxf(bm, fmaxf(x[t], x[t + 1]));
-                                b1 = fmaxf(b1, fmaxf(x[t + 2], x[t + 3]));
-                            }
-                            bm = fmaxf(bm, b1);
-                        }
-                    };
-                    if constexpr (KC == 32) {
-                        tmem_ld32(sc + rep * 32, v);
-                        tmem_ld_wait_regs(v);
-                        maximum(v, 0, 32);
-                    } else if constexpr (WIDE) {
-                        tmem_ld32(sc, v);
-                        tmem_ld32(sc + 32, v + 32);
-                        tmem_ld32(sc + 64, v2);
-                        tmem_ld32(sc + 96, v2 + 32);
-                        tmem_ld_wait_regs(v);
-                        tmem_ld_wait_regs(v + 32);
-                        tmem_ld_wait_regs(v2);
-                        tmem_ld_wait_regs(v2 + 32);
-                        maximum(v, 0, 64);
-                        maximum(v2, 64, 64);
+                        for (int t = 0; t < MINE; ++t)
+                            if (t >= limit) v[t] = none;
+                    }
+                    if (c < 0.f) {
+#pragma unroll
+                        for (int t = 0; t < MINE; ++t) bm = fminf(bm, v[t]);
                     } else {
-                        // with a whole row per thread: keys 0..63, then 64..127, which stay in registers
+                        float b1 = none;
 #pragma unroll
-                        for (int half = 0; half < KC / 64; ++half) {
-                            tmem_ld32(sc + rep * KC + half * 64, v);
-                            tmem_ld32(sc + rep * KC + half * 64 + 32, v + 32);
-                            tmem_ld_wait_regs(v);
-                            tmem_ld_wait_regs(v + 32);
-                            maximum(v, half * 64, 64);
+                        for (int t = 0; t < MINE; t += 4) {
+                            bm = fmaxf(bm, fmaxf(v[t], v[t + 1]));
+                            b1 = fmaxf(b1, fmaxf(v[t + 2], v[t + 3]));
                         }
+                        bm = fmaxf(bm, b1);
                     }
                     if (TWO && !(ok = wait_all(&turn[s], (done & 1) ^ (s == 0)))) break;       // the other stream is through with its exponentials
                     const float bmc = bm * c;
                     const bool raise = bmc > mc + kRaise || (mc == -INFINITY && bmc > -INFINITY);
-                    const bool shrink = raise && i > 0;
+                    const bool shrink = raise && u > 0;
                     const float f = shrink ? ex2_approx(mc - bmc) : 1.f;       // (a row without a finite score so far: its sum is zero)
                     if (raise) mc = bmc;
                     l *= f;
@@ -545,45 +540,26 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                             typename Pack2<T>::type h2 = Pack2<T>::down(e0, e1);
                             packed[t] = *reinterpret_cast<uint32_t*>(&h2);
                         }
-                        tmem_st16(sc + col, packed);
+                        tmem_st16(col, packed);
                     };
-                    if (KC < 128) {
+                    if constexpr (KC < 128) {
                         const uint32_t zeros[16] = {};
 #pragma unroll
                         for (int q = 0; q < 4; ++q)                // the other copies' keys
                             if (q / (KC / 32) != rep) tmem_st16(sc + (q >> 1) * 64 + (q & 1) * 16, zeros);
                     }
-                    if constexpr (KC == 32) {
-                        probabilities(v, (rep >> 1) * 64 + (rep & 1) * 16);
-                    } else if constexpr (KC == 64) {
-                        probabilities(v, rep * 64);
-                        probabilities(v + 32, rep * 64 + 16);
-                    } else if constexpr (WIDE) {
-                        probabilities(v, 0);
-                        probabilities(v + 32, 16);
-                        probabilities(v2, 64);
-                        probabilities(v2 + 32, 80);
-                    } else {
-                        // (columns 64..95 held scores that have just been read, columns 0..31 are written behind the reads of theirs)
-                        probabilities(v, 64);
-                        probabilities(v + 32, 80);
-                        tmem_ld32(sc, v);
-                        tmem_ld32(sc + 32, v + 32);
-                        tmem_ld_wait_regs(v);
-                        tmem_ld_wait_regs(v + 32);
-                        if (limit < 64) {
 #pragma unroll
-                            for (int t = 0; t < 64; ++t)
-                                if (t >= limit) v[t] = none;
-                        }
-                        probabilities(v, 0);
-                        probabilities(v + 32, 16);
+                    for (int t = 0; t < MINE; t += 32) {
+                        const int q = (h * HK + rep * KC + t) / 32;            // which 32 of the tile's keys
+                        probabilities(v + t, sc + (q >> 1) * 64 + (q & 1) * 16);
                     }
                     l += l0 + l1;
                     __syncwarp();
                     if (TWO && lane == 0) mbar_arrive(&turn[s ^ 1]);
                     if (__any_sync(0xffffffffu, shrink)) {
-                        // (the previous second product of this stream was done before these scores were made)
+                        // the stream's previous second product has to be done (with one buffer it was before these scores were made)
+                        if (HV == 2 && !(ok = wait_all(&pv_done[s][h ^ 1], (seen[h ^ 1] - 1) & 1))) break;
+                        tc_fence_after();
 #pragma unroll
                         for (int ch = 0; ch < HD / 32; ++ch) {
                             float o[32];
@@ -601,7 +577,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     if (lane == 0) mbar_arrive(&turn[s ^ 1]);
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[s]);
+                if (lane == 0) mbar_arrive(&p_full[s][h]);
             }
             if (!ok) break;
             // ---- the part goes out ----
@@ -629,7 +605,10 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 weight = m == -INFINITY ? 1.f : ex2_approx(mc - mb);
             }
             if (whole) weight *= 1.f / sum;
-            if (!(ok = wait_all(&pv_done[s], (done - 1) & 1))) break;
+            {
+                const int h = (units - 1) % HV;                    // (the last second product's end is all products' end)
+                if (!(ok = wait_all(&pv_done[s][h], (seen[h] - 1) & 1))) break;
+            }
             if (!idle) tc_fence_after();
 #pragma unroll
             for (int round = 0; round < 2; ++round) {
