@@ -630,23 +630,33 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     if (lane == 0) mbar_arrive(&o_empty[s]);
                 }
                 if (!(ok = group_sync())) break;                   // the stream's rows are in the room
-#pragma unroll 2
-                for (int k = 0; k < ITEMS; ++k) {
-                    const int i = k * 128 + (tid & 127), rt = i / CH4, e = i % CH4, r = row0 + base0 + rt;
-                    if (r >= R) break;
-                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                // a thread has chunk e of rows rt0, rt0 + 128 / CH4, ..., four of them under way together
+                constexpr int BATCH = ITEMS < 4 ? ITEMS : 4;
+                const int e = tid % CH4, rt0 = (tid & 127) / CH4;
+#pragma unroll 1
+                for (int k0 = 0; k0 < ITEMS && row0 + base0 + rt0 + k0 * (128 / CH4) < R; k0 += BATCH) {
+                    float4 x[BATCH];
+                    uint64_t to[BATCH];
 #pragma unroll
-                    for (int q = 0; q < REP; ++q) {
-                        const float4 y = reinterpret_cast<const float4*>(room + (q * ROWS + rt) * ROUND)[e ^ (rt & 7)];
-                        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                    for (int k = 0; k < BATCH; ++k) {
+                        const int rt = rt0 + (k0 + k) * (128 / CH4);
+                        x[k] = reinterpret_cast<const float4*>(room + rt * ROUND)[e ^ (rt & 7)];
+                        to[k] = whole ? row_o[part & 1][s][rt] : reinterpret_cast<uint64_t>(a.partial + (slot * ROWS + base0 + rt) * HD);
+#pragma unroll
+                        for (int q = 1; q < REP; ++q) {
+                            const float4 y = reinterpret_cast<const float4*>(room + (q * ROWS + rt) * ROUND)[e ^ (rt & 7)];
+                            x[k].x += y.x; x[k].y += y.y; x[k].z += y.z; x[k].w += y.w;
+                        }
                     }
-                    const int col = round * ROUND + 4 * e;
-                    if (whole) {
-                        typename Pack2<T>::type lo = Pack2<T>::down(x.x, x.y), hi = Pack2<T>::down(x.z, x.w);
-                        *reinterpret_cast<uint2*>(reinterpret_cast<T*>(row_o[part & 1][s][rt]) + col) =
-                            make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
-                    } else {
-                        *reinterpret_cast<float4*>(a.partial + (slot * ROWS + base0 + rt) * HD + col) = x;
+#pragma unroll
+                    for (int k = 0; k < BATCH; ++k) {
+                        if (row0 + base0 + rt0 + (k0 + k) * (128 / CH4) >= R) continue;
+                        if (whole) {
+                            typename Pack2<T>::type lo = Pack2<T>::down(x[k].x, x[k].y), hi = Pack2<T>::down(x[k].z, x[k].w);
+                            reinterpret_cast<uint2*>(to[k])[round * CH4 + e] = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+                        } else {
+                            reinterpret_cast<float4*>(to[k])[round * CH4 + e] = x[k];
+                        }
                     }
                 }
                 if (round == 0 && !(ok = group_sync())) break;     // the room is read
