@@ -12,7 +12,8 @@
 //                 share of a tile's keys (the probabilities of the others are zeros): what a thread has to do for a tile, which is what
 //                 few rows wait for, is a half or a quarter.  The copies are added up at the end.
 //   ROWS = 256    the streams are two tiles of 128 rows over the same keys, and take turns in their exponentials: at the same time, they
-//                 would only get half of the special function units each, and then both wait for the tensor pipe.
+//                 would only get half of the special function units each, and then both wait for the tensor pipe (512 rows over 512 keys
+//                 63.4 us in turns, 67.1 without; longer ones the same).
 // Where a thread has a whole row (128 or 256 rows) a stream has two score buffers of 64 keys, and the scores of one are made while the
 // probabilities of the other are: a thread's chain is its exponentials alone.
 // The reference maximum of a row follows a tile's maximum only when that exceeds it by more than 2^8 (probabilities up to 256
@@ -27,12 +28,12 @@
 //   by cp.async      warps 8-11 keys and values (ROWS <= 128: two a stream), warps 12, 13 products
 // The softmax warps bring the queries themselves, when a part begins: their room is the one that the previous part has left through.
 //
-// 32 rows of 32 heads of 16 sequences of 384 to 704 keys (143 MB): 44.9 us, 3.4 TB/s; bound by the chain a short item is (queries, first
-// scores, exponentials, second product, way out: 15 us for its four tiles), which two streams hide half of.  Before: 59.5 us on
+// 32 rows of 32 heads of 16 sequences of 384 to 704 keys (143 MB): 45 us, 3.3 TB/s; bound by the chain a short item is (queries, first
+// scores, exponentials, second product, way out: 10 us for its four tiles), which two streams hide half of.  Before: 59.5 us on
 // mma.sync in tiles of 32 rows, 66 as one stream of even and odd tiles, which ended its items together.
-// 224 rows a key head of eight sequences of 2001 to 9001 keys (20 GFLOP): 53 us, 380 TFLOP/s; bound by a tile's chain (exponentials 2.4k
-// cycles, of which a quarter waits for stores to tensor memory, and the two products 1.9k) and by the parts' ends; 104 us on mma.sync.  256
-// rows of 704 over 704 keys: 557 TFLOP/s.
+// 224 rows a key head of eight sequences of 2001 to 9001 keys (20 GFLOP): 49 us, 410 TFLOP/s; bound by the exponentials' chain (1.45k cycles for
+// 64 keys of 128 rows, 0.6k of them until the stores to tensor memory are done, which share it with the other products) and by start and end
+// of a part (8k cycles); 104 us on mma.sync, 51.5 with one score buffer of 128 keys.  704 rows over 704 keys: 630 TFLOP/s.
 //
 // Every barrier is waited on phase by phase by whoever waits on it, so that a parity says which phase is meant.  All waits end: one
 // that gives up makes the CTA leave, after its copies and products under way have ended.
