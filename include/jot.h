@@ -388,12 +388,12 @@ typedef struct {
  * d_positions[row] (int32; negative: padding), rounded once.  k may be NULL.  With pages, k's results go to the pages of
  * `layer` at d_slots[row] = page * page_size + offset (k->out is ignored), and v (not NULL then; in, strides and n_heads
  * count) is copied beside them; a negative slot writes neither.  Slots must differ: where two rows name one slot,
- * which of them it holds is not defined.  8 <= head_dim <= 256. */
+ * which of them it holds is not defined.  8 <= head_dim <= 256; at most 2^31 - 4097 rows and 2^29 - 1 heads a kind. */
 int jot_head_norm_rope(const jot_heads* q, const jot_heads* k, const jot_rope* rope, int dtype, int n_rows, int head_dim,
                        float eps, const int32_t* d_positions, const jot_heads* v, const jot_kv_pages* pages, int layer,
                        const int32_t* d_slots, int32_t* d_status, void* stream);
 
-/* Rows of keys and values [n_rows, n_kv_heads, head_dim] into the pages of one layer, as above. */
+/* Rows of keys and values [n_rows, n_kv_heads, head_dim] into the pages of one layer, as above (at most 2^31 - 4097 rows). */
 int jot_kv_write(const jot_kv_pages* pages, int layer, int n_rows, const void* d_k, int64_t k_row_stride,
                  int64_t k_head_stride, const void* d_v, int64_t v_row_stride, int64_t v_head_stride,
                  const int32_t* d_slots, int32_t* d_status, void* stream);

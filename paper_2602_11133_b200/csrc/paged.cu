@@ -21,6 +21,9 @@ namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// Rows and heads are counted in 31 bits, the grid's last CTA and a row's last stretch of heads (queries, keys and values) included.
+constexpr int kMostRows = INT32_MAX - 4096, kMostHeads = INT32_MAX / 4;
+
 // A stride counts only where there is a second element along it.
 bool stride_ok(int64_t s, int64_t n) { return n <= 1 || s % 8 == 0; }
 
@@ -264,6 +267,7 @@ int jot_head_norm_rope(const jot_heads* q, const jot_heads* k, const jot_rope* r
     if (n_rows == 0) return JOT_OK;
     JOT_TRY(check_heads(q, n_rows, true));
     if (k) JOT_TRY(check_heads(k, n_rows, !pages));
+    if (n_rows > kMostRows || q->n_heads > kMostHeads || (k && k->n_heads > kMostHeads)) return JOT_ERR_SHAPE;
     HeadArgs a{};
     if (pages) {
         JOT_TRY(check_heads(v, n_rows, false));
@@ -299,6 +303,7 @@ int jot_kv_write(const jot_kv_pages* pages, int layer, int n_rows, const void* d
     if (!stride_ok(k_row_stride, n_rows) || !stride_ok(v_row_stride, n_rows) || !stride_ok(k_head_stride, pages->n_kv_heads) ||
         !stride_ok(v_head_stride, pages->n_kv_heads))
         return JOT_ERR_ARG;
+    if (n_rows > kMostRows) return JOT_ERR_SHAPE;
     DeviceInfo* di = nullptr;
     JOT_TRY(device_info(&di));
     WriteArgs a{};

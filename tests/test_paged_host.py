@@ -73,6 +73,17 @@ def test_head_norm_rope_refusals(jot):
     assert call(pages=p, k=H(), v=H(), slots=PTR, layer=1) == ARG
 
 
+def test_counts_beyond_31_bits_are_refused(jot):
+    # the kernels count rows and heads in 31 bits, up to the end of the last CTA's rows
+    lib, p, most = jot._lib(), pages_struct(jot), 2 ** 31 - 1
+    heads = lambda n: jot._pack_heads(PTR, 8, 8, PTR, 8, 8, 0, n)
+    rope = jot._pack_rope(0, 0, 0, 1.0)
+    assert lib.jot_head_norm_rope(heads(1), None, rope, 0, most, 8, 1e-6, PTR, None, None, 0, None, None, None) == SHAPE
+    assert lib.jot_head_norm_rope(heads(most), None, rope, 0, 1, 8, 1e-6, PTR, None, None, 0, None, None, None) == SHAPE
+    assert lib.jot_head_norm_rope(heads(1), heads(most), rope, 0, 1, 8, 1e-6, PTR, None, None, 0, None, None, None) == SHAPE
+    assert lib.jot_kv_write(p, 0, most, PTR, 256, 64, PTR, 256, 64, PTR, None, None) == SHAPE
+
+
 def test_copy_lists_that_hang_on_their_order_are_refused(jot):
     lib, p = jot._lib(), pages_struct(jot, n_pages=100)
 
