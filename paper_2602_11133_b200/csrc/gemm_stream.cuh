@@ -200,7 +200,7 @@ gemm_stream_partial_kernel(const GemmParams p, const __grid_constant__ CUtensorM
         tc_fence_after();
         tmem_dealloc_pair(tmem_base, tmem_cols);
     }
-    if (threadIdx.x == 0 && abort_flag && p.status) atomicExch(p.status, 6);
+    if (threadIdx.x == 0 && abort_flag && p.status) atomicExch(p.status, 8);     // (5 and 6 are the caller's input)
 }
 
 // ---------------------------------------------------------------- gate/up + SwiGLU

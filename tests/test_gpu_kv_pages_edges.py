@@ -1,0 +1,47 @@
+"""The model's cache where it can go wrong: attached while a stream is busy, filled by a pass that failed, its status word."""
+import pytest
+import torch
+
+from paper_2602_11133_b200 import inputs
+from test_gpu_kv_pages import in_pages, jot  # noqa: F401 (jot: the fixture)
+from test_gpu_kvcache import GEOMS
+
+pytestmark = pytest.mark.gpu
+
+
+def small(jot, B=2, P=40, G=56, name="gqa"):
+    g = GEOMS[name]
+    model = jot.Model(g, inputs.weights_to(inputs.model_weights(g, seed=0), "cuda"), B, P + G)
+    canvas = inputs.partially_masked_canvas(1, B, P, G, g.vocab, g.mask_id, 0.8)
+    canvas[:, P:P + 16] = g.mask_id
+    return g, model, canvas.cuda(), P, P + 16
+
+
+def control(model):
+    """The model's status word."""
+    at = -model.workspace.data_ptr() % 1024
+    return model.workspace[at:at + 4].view(torch.int32)
+
+
+def refused(jot, status, fn):
+    with pytest.raises(jot.JotError) as e:
+        fn()
+    assert e.value.status == status
+
+
+@pytest.mark.parametrize("word,status", [(1, -5), (2, -5), (3, -5), (4, -5), (7, -5), (8, -5), (5, -1), (6, -1)])
+def test_what_the_status_words_of_the_kernels_mean(jot, word, status):
+    _, model, _, _, _ = small(jot)
+    control(model).fill_(word)
+    refused(jot, status, model.read_status)
+    # what the caller can mend is taken off the record, an expired wait stays
+    assert int(control(model)) == (0 if status == -1 else word)
+    model.close()
+
+
+def busy_block(nbytes):
+    """On the current stream: a block of memory that a queued kernel will still write when the block is already free again."""
+    block = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    torch.cuda._sleep(400_000_000)                                 # some 0.2 s
+    block.fill_(0x55)
+    return block.data_ptr()
