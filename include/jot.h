@@ -347,8 +347,8 @@ int jot_gemm_bf16_noalloc(const void* d_A, const void* d_W, const void* d_residu
  *   - A negative position, slot or length marks padding: what belongs to it stays as it was.
  *   - Slots, page numbers and lengths live on the device and are checked there: what lies outside the pages is never
  *     read or written (a slot is skipped; a page reads as zeros; a length counts up to the end of the table's row), and
- *     *d_status (int32, nullable, never reset) becomes JOT_STATUS_BAD_INDEX.  (2 there: a bounded wait on the device expired; the
- *     call's outputs are undefined.)
+ *     *d_status (int32, nullable, never reset) becomes JOT_STATUS_BAD_INDEX unless it is positive already.  (2 there: a bounded wait on
+ *     the device expired; the call's outputs are undefined.)
  *   - Nothing is allocated and nothing synchronises; the calls may be captured into a CUDA graph. */
 enum { JOT_BF16 = 0, JOT_FP16 = 1 };
 enum { JOT_STATUS_BAD_INDEX = 6 };

@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_norm_rope_kernel(const H
     if (a.to_pages && slot >= 0) {
         const int page = slot / a.pages.page_size, off = slot - page * a.pages.page_size;
         if (page >= a.pages.n_pages) {
-            if (group == r * per_row && sub == 0 && a.status) atomicExch(a.status, kStatusBadIndex);
+            if (group == r * per_row && sub == 0 && a.status) report_bad_index(a.status);
             slot = -1;
         } else {
             k_at = page * a.pages.k_page + (int64_t)off * a.head_dim;

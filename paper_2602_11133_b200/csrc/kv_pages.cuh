@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kMoveThreads) kv_write_kernel(const WriteArgs 
         const int slot = a.slots[row], page = slot / a.pages.page_size;
         if (slot < 0) continue;
         if (page >= a.pages.n_pages) {
-            if (in_row == 0 && a.status) atomicExch(a.status, kStatusBadIndex);
+            if (in_row == 0 && a.status) report_bad_index(a.status);
             continue;
         }
         const uint4 kv = reinterpret_cast<const uint4*>(a.k + row * a.k_row + h * a.k_head)[c];
@@ -51,7 +51,7 @@ __global__ void page_rows_kernel(const int32_t* __restrict__ table, int64_t tabl
     positions[r] = pos;
     const bool real = (unsigned)page < (unsigned)n_pages;
     slots[r] = real ? page * page_size + pos - p * page_size : -1;
-    if (!real) atomicExch(status, kStatusBadIndex);
+    if (!real) report_bad_index(status);
 }
 
 // The pairs travel as kernel arguments, as the caller's lists live on the host and may change right after the call.

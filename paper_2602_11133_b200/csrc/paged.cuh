@@ -10,6 +10,12 @@ namespace jot {
 
 constexpr int32_t kStatusBadIndex = 6;     // status word: a slot, a page or a length outside the pages (skipped, or read as zeros)
 
+// Puts a bad index on record, unless an expired wait is there already, which says more.
+__device__ __forceinline__ void report_bad_index(int32_t* status) {
+    const int32_t held = *reinterpret_cast<volatile int32_t*>(status);
+    if (held <= 0) atomicCAS(status, held, kStatusBadIndex);
+}
+
 // Whether the kernels can work on these pages.
 int check_kv_pages(const jot_kv_pages* pages, int layer);
 // Positions, slots and lengths of a pass over positions pos0 .. pos0 + rows_per_seq - 1 of B canvases of L positions, whose pages are

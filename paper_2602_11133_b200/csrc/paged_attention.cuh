@@ -128,7 +128,7 @@ __device__ __forceinline__ PagedRange paged_range(const PagedArgs& a, int tile, 
         if (b >= a.B) return 0;
         const int n = paged_len(a, b);
         empty |= n == 0;
-        if (blockIdx.x == 0 && a.status && a.lens[b] > (int64_t)a.max_pages * a.pages.page_size) atomicExch(a.status, kStatusBadIndex);
+        if (blockIdx.x == 0 && a.status && a.lens[b] > (int64_t)a.max_pages * a.pages.page_size) report_bad_index(a.status);
         return n > 0 ? (a.whole ? per_b : (n + tile - 1) / tile * per_b) : 0;
     };
     auto scan = [&](int v) {        // inclusive, over the warp
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
             if ((unsigned)page < (unsigned)a.pages.n_pages)
                 at = reinterpret_cast<uint64_t>(pages + page * page_stride + (int64_t)in_page * HD);
             else if (a.status)
-                atomicExch(a.status, kStatusBadIndex);
+                report_bad_index(a.status);
         }
         row_at[buf][tid] = at;
     };

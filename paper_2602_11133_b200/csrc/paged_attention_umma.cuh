@@ -248,7 +248,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                     const bool real = lane < here;
                     int pg = page;
                     if (real && (unsigned)pg >= (unsigned)a.pages.n_pages) {
-                        if (a.status) atomicExch(a.status, kStatusBadIndex);
+                        if (a.status) report_bad_index(a.status);
                         pg = a.pages.n_pages;                      // past the map's end: zeros
                     }
                     const int off = ps <= 128 ? 0 : key % ps;
@@ -328,7 +328,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                             ka = reinterpret_cast<uint64_t>((const T*)a.pages.k + page[i] * a.pages.k_page + (int64_t)in_page[i] * HD);
                             va = reinterpret_cast<uint64_t>((const T*)a.pages.v + page[i] * a.pages.v_page + (int64_t)in_page[i] * HD);
                         } else if (a.status) {
-                            atomicExch(a.status, kStatusBadIndex);
+                            report_bad_index(a.status);
                         }
                     }
                     at[buf][pt + i * PW * 32] = ka;

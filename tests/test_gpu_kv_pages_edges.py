@@ -39,6 +39,16 @@ def test_what_the_status_words_of_the_kernels_mean(jot, word, status):
     model.close()
 
 
+def test_a_bad_page_does_not_take_an_expired_wait_off_the_record(jot):
+    g, model, canvas, lo, hi = small(jot)
+    _, table = in_pages(jot, model, g, 2, canvas.shape[1], 16)
+    model.denoise_step_cached(canvas, lo, hi, refresh=True)
+    control(model).fill_(3)
+    table[1, 0] = 10 ** 6
+    refused(jot, -5, lambda: model.denoise_step_cached(canvas, lo, hi, refresh=False))
+    model.close()
+
+
 def busy_block(nbytes):
     """On the current stream: a block of memory that a queued kernel will still write when the block is already free again."""
     block = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
