@@ -56,9 +56,14 @@ struct PagedArgs {
     int4* desc;                             // (sequence, item within it, parts, share it begins in); parts 0: not cut
     bool by_item;                           // one per item (there are at most as many as shares), else one per share: the item that begins there
     float* partial;                         // [CTA][2][MT][HD] unnormalised outputs
-    float2* partial_ml;                     // [CTA][2][MT] (maximum in base 2, sum)
+    float2* partial_ml;                     // [CTA][2][MT] (reference of the exponentials in base 2, sum)
     int32_t* status;
 };
+
+// fp16 has no number below 2^-24: a row's exponentials are taken against a reference this far (in base 2) below its maximum, so that keys of 2^-25
+// of the leading one and less, of which a long cache has many, count in the product as they do in the sum.  (tcgen05 lets probabilities grow by 2^8
+// more before the reference follows: 2^15 together, and fp16 ends at 65504.)  The stored maximum of a part is its reference.
+template <typename T> constexpr float kPagedLift = PackIsBf16<T>::value ? 0.f : 7.f;
 
 template <typename T> struct MmaOp;
 template <> struct MmaOp<__nv_bfloat16> {
@@ -410,11 +415,11 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
                 top[hh] = fmaxf(top[hh], __shfl_xor_sync(0xffffffffu, top[hh], 1));
                 top[hh] = fmaxf(top[hh], __shfl_xor_sync(0xffffffffu, top[hh], 2));
             }
-            float base[2] = {top[0] == -INFINITY ? 0.f : top[0], top[1] == -INFINITY ? 0.f : top[1]};   // no key yet: all exponentials are zero
+            float base[2] = {top[0] == -INFINITY ? 0.f : top[0] - kPagedLift<T>, top[1] == -INFINITY ? 0.f : top[1] - kPagedLift<T>};   // no key yet: all exponentials are zero
             if (__any_sync(0xffffffffu, top[0] != mx[0] || top[1] != mx[1])) {
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
-                    const float f = ex2_approx(mx[hh] - base[hh]);
+                    const float f = ex2_approx(mx[hh] - kPagedLift<T> - base[hh]);
                     mx[hh] = top[hh];
                     sum[hh] *= f;
 #pragma unroll
@@ -454,6 +459,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
         for (int hh = 0; hh < 2; ++hh) {
             sum[hh] += __shfl_xor_sync(0xffffffffu, sum[hh], 1);
             sum[hh] += __shfl_xor_sync(0xffffffffu, sum[hh], 2);
+            mx[hh] -= kPagedLift<T>;                                    // from here on the reference
             if (t4 == 0) ml[warp][g + 8 * hh] = make_float2(mx[hh], sum[hh]);
         }
         __syncthreads();

@@ -16,8 +16,8 @@
 //                 63.4 us in turns, 67.1 without; longer ones the same).
 // Where a thread has a whole row (128 or 256 rows) a stream has two score buffers of 64 keys, and the scores of one are made while the
 // probabilities of the other are: a thread's chain is its exponentials alone.
-// The reference maximum of a row follows a tile's maximum only when that exceeds it by more than 2^8 (probabilities up to 256
-// are as exact as those up to 1); then the row of the accumulator is rescaled in tensor memory.
+// The reference of a row's exponentials, its maximum (in fp16 less kPagedLift), follows a tile's maximum only when that exceeds the one it was taken
+// from by more than 2^8 (probabilities up to 256 are as exact as those up to 1); then the row of the accumulator is rescaled in tensor memory.
 //
 // Pages of a multiple of 8 keys come by TMA (one box per page and 64 columns; a tile is as many whole pages as fit into 128 rows, or
 // 128 keys of a larger page), others by cp.async, 16 bytes a request, which costs four warps and the rate at which an SM takes
@@ -125,7 +125,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
     constexpr int HV = KC == 128 ? 2 : 1, HK = 128 / HV;          // score buffers of a stream, and keys of one
     constexpr uint32_t IDESC_S = umma_idesc16<T>(128, HK, false), IDESC_O = umma_idesc16<T>(128, HD, true);
     constexpr uint32_t O_COL = 256;              // scores of the streams at columns 0 and 128, accumulators at 256 and 384
-    constexpr float kRaise = 8.f;
+    constexpr float kRaise = 8.f + kPagedLift<T>;
 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -135,7 +135,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
         drain[2], turn[2], tail_bar, prod_bar[2], g_bar[2];
     __shared__ uint64_t row_at[TMA ? 1 : STREAMS][2][TMA ? 1 : 2 * TILE];      // by cp.async: addresses of a tile's key rows, then of its value rows; odd: no such row
     __shared__ uint64_t row_q[2][128], row_o[2][2][128];     // addresses of the rows' queries, and of their results ([parity of the part])
-    __shared__ float2 x_ml[2][REP > 1 ? 128 : 1];            // [stream][row] (maximum, sum) of the copies
+    __shared__ float2 x_ml[2][REP > 1 ? 128 : 1];            // [stream][row] (reference, sum) of the copies
     __shared__ PagedRangeSmem range_smem;
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag, drain_flag;
@@ -522,11 +522,11 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                         bm = fmaxf(bm, b1);
                     }
                     if (TWO && !(ok = wait_all(&turn[s], (done & 1) ^ (s == 0)))) break;       // the other stream is through with its exponentials
-                    const float bmc = bm * c;
-                    const bool raise = bmc > mc + kRaise || (mc == -INFINITY && bmc > -INFINITY);
+                    const float bmc = bm * c, ref = bmc - kPagedLift<T>;
+                    const bool raise = bmc - mc > kRaise;                      // (the first finite score, too: mc is minus infinity)
                     const bool shrink = raise && u > 0;
-                    const float f = shrink ? ex2_approx(mc - bmc) : 1.f;       // (a row without a finite score so far: its sum is zero)
-                    if (raise) mc = bmc;
+                    const float f = shrink ? ex2_approx(mc - ref) : 1.f;       // (a row without a finite score so far: its sum is zero)
+                    if (raise) mc = ref;
                     l *= f;
                     const float base = mc == -INFINITY ? 0.f : mc;
                     float l0 = 0.f, l1 = 0.f;
@@ -591,7 +591,7 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
             if (REP > 1) {
                 x_ml[s][r128] = make_float2(mc, l);
                 if (!(ok = group_sync())) break;
-                // maximum and sum over the copies
+                // reference and sum over the copies
                 const int rt = r128 % ROWS;
                 m = -INFINITY;
                 sum = 0.f;

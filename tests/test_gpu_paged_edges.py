@@ -39,3 +39,34 @@ def test_a_bad_index_does_not_take_an_expired_wait_off_the_record(jot):
                 status = int32([held])
                 call(status)
                 assert int(status) == want
+
+
+# ---------------------------------------------------------------------------------------------- numerics
+@pytest.mark.parametrize("page", [64, 10])
+@pytest.mark.parametrize("T,n", [(5, 2 ** 19), (20, 2 ** 19), (40, 2 ** 18), (80, 2 ** 17), (150, 2 ** 17)])
+def test_a_long_flat_tail_beside_one_key_that_leads(jot, T, n, page):
+    """One key in front of hundreds of thousands that each weigh just under 2^-25 of it, and 0.4 % to 1.6 % together: fp16's smallest number
+    is 2^-24, so that weights taken relative to the leading one vanish from the product while the sum counts them.  The leading value is 0
+    and the others 1: what comes out is the others' share.  As many sequences (over the same pages) as there are shares of the work, so
+    that none is cut into parts with maxima of their own; a warp's range of keys, or a copy of a row, has 2^17 of them."""
+    hd, seqs, lead_by = 64, 448, 25.0625
+    n_pages = (n + page - 1) // page
+    pages = jot.KVPages(torch.zeros(1, n_pages, 1, page, hd, dtype=FP16, device="cuda"), torch.ones(1, n_pages, 1, page, hd, dtype=FP16, device="cuda"))
+    q = torch.zeros(1, T, 1, hd, dtype=FP16, device="cuda")
+    q[..., 0] = 16
+    q, table, lens = q.expand(seqs, -1, -1, -1), torch.arange(n_pages, dtype=torch.int32, device="cuda")[None].expand(seqs, -1), int32([n] * seqs)
+    for lead in (0, n // 2 + 7):
+        pages.k.zero_()
+        pages.v.fill_(1)
+        pages.k[0, lead // page, 0, lead % page, 0] = lead_by / 16          # exact in fp16
+        pages.v[0, lead // page, 0, lead % page] = 0
+        lse = torch.empty(seqs, T, 1, device="cuda")
+        out = jot.paged_attention(q, pages, table, lens, scale=math.log(2), lse=lse)
+        tail = (n - 1) * 2.0 ** -lead_by
+        # The result's rounding: 2^-11.  A weight's: with the leading one at 2^7 the others are 2^-18.1, of which half of 2^-24 is 2^-6.9.  The sum,
+        # in fp32 beside the leading weight: every pair of the thread that has the leading key, half an ulp at each of 2^14 steps, 2^-10; the
+        # product's own sum holds nothing but such weights, with an ulp of 2^-23 lost at each of 2^13 steps of 16 keys: 2^-10
+        err = (out.double() - tail / (1 + tail)).abs().max().item()
+        assert err <= (2.0 ** -11 + 2.0 ** -6.9 + 2.0 ** -10 + 2.0 ** -10) * tail, (lead, err / tail)
+        want = lead_by * math.log(2) + math.log1p(tail)
+        assert ((lse.double() - want).abs() <= 2.0 ** -10 + 2.0 ** -20 + 2.0 ** -22 * want).all()
