@@ -521,21 +521,30 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                         }
                         bm = fmaxf(bm, b1);
                     }
-                    if (TWO && !(ok = wait_all(&turn[s], (done & 1) ^ (s == 0)))) break;       // the other stream is through with its exponentials
                     const float bmc = bm * c, ref = bmc - kPagedLift<T>;
                     const bool raise = bmc - mc > kRaise;                      // (the first finite score, too: mc is minus infinity)
                     const bool shrink = raise && u > 0;
                     const float f = shrink ? ex2_approx(mc - ref) : 1.f;       // (a row without a finite score so far: its sum is zero)
                     if (raise) mc = ref;
-                    l *= f;
                     const float base = mc == -INFINITY ? 0.f : mc;
+                    // Scores are scaled and taken off the reference in one fma, unrounded in between, and the reference is the maximum scaled and rounded:
+                    // beyond 2^20 the two would be apart by a fraction of an exponent first, by more than an exponent holds in the end.  Then scores
+                    // are rounded, too.  (The question costs 1 % at most: 224 rows of eight sequences 48.9 us without it, 49.2 with.)
+                    float step = c;
+                    if (__any_sync(0xffffffffu, fabsf(base) > 1048576.f)) {
+                        step = 1.f;
+#pragma unroll
+                        for (int t = 0; t < MINE; ++t) v[t] *= c;
+                    }
+                    if (TWO && !(ok = wait_all(&turn[s], (done & 1) ^ (s == 0)))) break;       // the other stream is through with its exponentials
+                    l *= f;
                     float l0 = 0.f, l1 = 0.f;
                     // 32 scores -> 16 columns of probabilities: keys 0..63 of the tile in columns 0..31, 64..127 in columns 64..95
                     auto probabilities = [&](const float* x, uint32_t col) {
                         uint32_t packed[16];
 #pragma unroll
                         for (int t = 0; t < 16; ++t) {
-                            const float e0 = ex2_approx(fmaf(x[2 * t], c, -base)), e1 = ex2_approx(fmaf(x[2 * t + 1], c, -base));
+                            const float e0 = ex2_approx(fmaf(x[2 * t], step, -base)), e1 = ex2_approx(fmaf(x[2 * t + 1], step, -base));
                             l0 += e0;
                             l1 += e1;
                             typename Pack2<T>::type h2 = Pack2<T>::down(e0, e1);

@@ -70,3 +70,27 @@ def test_a_long_flat_tail_beside_one_key_that_leads(jot, T, n, page):
         assert err <= (2.0 ** -11 + 2.0 ** -6.9 + 2.0 ** -10 + 2.0 ** -10) * tail, (lead, err / tail)
         want = lead_by * math.log(2) + math.log1p(tail)
         assert ((lse.double() - want).abs() <= 2.0 ** -10 + 2.0 ** -20 + 2.0 ** -22 * want).all()
+
+
+@pytest.mark.parametrize("page", [16, 10])
+@pytest.mark.parametrize("dtype,size", [(FP16, 4000.0), (FP16, 60000.0), (BF16, 30000.0), (BF16, 2.0 ** 40)])
+@pytest.mark.parametrize("T", ROWS)
+def test_scores_of_which_fp32_holds_no_fraction(jot, T, dtype, size, page):
+    """Scores of 10^8 and more, alike or far apart: the leading keys share the weight evenly."""
+    n, hd = 300, 128
+    pages, table = spread(jot, 3, [n], 1, page, hd, dtype)
+    q = torch.full((1, T, 1, hd), size, dtype=dtype, device="cuda")
+    ids = table[0, :(n + page - 1) // page].long().cuda()
+    values = pages.v[0][ids, 0].reshape(-1, hd)[:n].double()
+    for small, sign in ((0, 1), (200, 1), (200, -1)):                       # so many keys of zeros in front, whose weight is zero
+        keys = torch.zeros(len(ids) * page, hd, dtype=dtype, device="cuda")
+        keys[small:n] = sign * size
+        pages.k[0, ids] = keys.view(len(ids), 1, page, hd)
+        lse = torch.empty(1, T, 1, device="cuda")
+        out = jot.paged_attention(q, pages, table.cuda(), int32([n]), scale=sign * hd ** -0.5, lse=lse)[0, :, 0].double()
+        want, total = values[small:].mean(0), values[small:].abs().mean(0)
+        # alike scores have alike weights, powers of two apart from the rescaling of sums: no rounding of a weight but its own
+        tol = torch.finfo(dtype).eps / 2 * (want.abs() + total) + 2.0 ** -18 * total
+        assert ((out - want).abs() <= tol).all(), (small, sign, out[0, :3], want[:3])
+        top = float(torch.tensor(size, dtype=dtype).double() ** 2 * hd) * hd ** -0.5
+        assert ((lse.double() - top).abs() <= 2.0 ** -20 * top).all()
