@@ -380,8 +380,8 @@ int jot_paged_attention(const void* d_q, int64_t q_seq_stride, int64_t q_row_str
     a.B = B; a.T = T; a.nq = n_q_heads; a.nkv = pages->n_kv_heads; a.group = group;
     a.pages = layer_pages(pages, layer);
     a.table = d_page_table; a.table_stride = table_stride; a.max_pages = max_pages; a.lens = d_lens;
-    // (a scale of zero as the smallest normal number: every score is zero all the same, and a key that is not there stays at minus infinity)
-    a.scale_log2 = scale == 0.f ? FLT_MIN : scale * 1.4426950408889634f;
+    // (a scale of zero as the smallest number there is: every score is as good as zero all the same, and a key that is not there stays at minus infinity)
+    a.scale_log2 = scale == 0.f ? FLT_TRUE_MIN : scale * 1.4426950408889634f;
     uint8_t* ws = (uint8_t*)d_workspace;
     a.desc = (int4*)(ws + sp.desc); a.partial_ml = (float2*)(ws + sp.ml); a.partial = (float*)(ws + sp.partial);
     a.status = d_status;

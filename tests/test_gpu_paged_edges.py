@@ -94,3 +94,20 @@ def test_scores_of_which_fp32_holds_no_fraction(jot, T, dtype, size, page):
         assert ((out - want).abs() <= tol).all(), (small, sign, out[0, :3], want[:3])
         top = float(torch.tensor(size, dtype=dtype).double() ** 2 * hd) * hd ** -0.5
         assert ((lse.double() - top).abs() <= 2.0 ** -20 * top).all()
+
+
+@pytest.mark.parametrize("T", ROWS)
+def test_a_scale_of_zero_gives_the_mean_of_the_values(jot, T):
+    n, hd = 200, 64
+    for dtype, size in ((BF16, 1.0), (FP16, 1.0), (BF16, 2.0 ** 60)):       # scores of up to 2^126, times zero
+        pages, table = spread(jot, 7, [n], 1, 16, hd, dtype)
+        pages.k.mul_(size)
+        q = normal(9, (1, T, 1, hd), dtype) * size
+        ids = table[0, :13].long().cuda()
+        v = pages.v[0][ids, 0].reshape(-1, hd)[:n].double()
+        lse = torch.empty(1, T, 1, device="cuda")
+        for scale in (0.0, -0.0):
+            out = jot.paged_attention(q, pages, table.cuda(), int32([n]), scale=scale, lse=lse)[0, :, 0].double()
+            tol = torch.finfo(dtype).eps / 2 * (v.mean(0).abs() + v.abs().mean(0)) + 2.0 ** -18 * v.abs().mean(0)
+            assert ((out - v.mean(0)).abs() <= tol).all()
+            assert ((lse.double() - math.log(n)).abs() <= 2.0 ** -20 + 2.0 ** -22 * math.log(n)).all()
