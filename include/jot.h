@@ -407,8 +407,8 @@ int jot_kv_copy_pages(const jot_kv_pages* pages, int n, const int32_t* src, cons
 /* Attention of T rows per sequence over the sequence's keys in the pages of `layer`: key j of sequence b is in page
  * d_page_table[b * table_stride + j / page_size] at offset j % page_size, j < d_lens[b].  Every row sees every key
  * (bidirectional).  q and out [B, T, n_q_heads, head_dim] with strides (sequence, row, head); query head h uses key head
- * h / (n_q_heads / n_kv_heads).  d_lse (nullable, [B, T, n_q_heads] fp32): ln of the sum of exp(scale * q . k).  A length of 0
- * gives zeros and -inf.  head_dim 64 or 128.  Fewer than 2^31 tiles of 64 keys over all sequences, heads and rows, were every
+ * h / (n_q_heads / n_kv_heads).  d_lse (nullable, [B, T, n_q_heads] fp32): ln of the sum of exp(scale * q . k);
+ * scale times log2(e) is finite (JOT_ERR_ARG otherwise).  A length of 0 gives zeros and -inf.  head_dim 64 or 128.  Fewer than 2^31 tiles of 64 keys over all sequences, heads and rows, were every
  * sequence as long as its table row allows.  Entries of a table row past its length are not read.  Tokens past a length within
  * a page may hold anything, NaN included.
  * d_workspace: at least jot_paged_attention_workspace_bytes() (0 on invalid arguments), 16-byte aligned, the call's own until it

@@ -359,7 +359,9 @@ int jot_paged_attention(const void* d_q, int64_t q_seq_stride, int64_t q_row_str
         !stride_ok(out_row_stride, T) || !stride_ok(out_head_stride, n_q_heads))
         return JOT_ERR_ARG;
     if (n_q_heads % pages->n_kv_heads || (pages->head_dim != 64 && pages->head_dim != 128)) return JOT_ERR_SHAPE;
-    if (!(scale == scale) || std::isinf(scale)) return JOT_ERR_ARG;
+    // (a scale of zero as the smallest number there is: every score is as good as zero all the same, and a key that is not there stays at minus infinity)
+    const float scale_log2 = scale == 0.f ? FLT_TRUE_MIN : scale * 1.4426950408889634f;
+    if (!std::isfinite(scale_log2)) return JOT_ERR_ARG;
     const int group = n_q_heads / pages->n_kv_heads;
     const int64_t rows = (int64_t)T * group;
     if (rows > INT32_MAX / 256 || (int64_t)T * n_q_heads > INT32_MAX / 32) return JOT_ERR_SHAPE;
@@ -380,8 +382,7 @@ int jot_paged_attention(const void* d_q, int64_t q_seq_stride, int64_t q_row_str
     a.B = B; a.T = T; a.nq = n_q_heads; a.nkv = pages->n_kv_heads; a.group = group;
     a.pages = layer_pages(pages, layer);
     a.table = d_page_table; a.table_stride = table_stride; a.max_pages = max_pages; a.lens = d_lens;
-    // (a scale of zero as the smallest number there is: every score is as good as zero all the same, and a key that is not there stays at minus infinity)
-    a.scale_log2 = scale == 0.f ? FLT_TRUE_MIN : scale * 1.4426950408889634f;
+    a.scale_log2 = scale_log2;
     uint8_t* ws = (uint8_t*)d_workspace;
     a.desc = (int4*)(ws + sp.desc); a.partial_ml = (float2*)(ws + sp.ml); a.partial = (float*)(ws + sp.partial);
     a.status = d_status;
