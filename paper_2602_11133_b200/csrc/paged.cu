@@ -111,7 +111,7 @@ int launch_join(const PagedArgs& a, int shares, int row_tile, cudaStream_t st) {
     const int rows = std::min(row_tile, a.T * a.group);
     const int64_t items = paged_items(a, row_tile);
     const int grid = a.by_item ? (int)items : shares;
-    auto go = [&](auto* kernel, int per_cta) { launch_k(kernel, dim3((unsigned)grid, (unsigned)((rows + per_cta - 1) / per_cta)), dim3(kPagedThreads), 0, st, a, row_tile); };
+    auto go = [&](auto* kernel, int per_cta) { launch_k(kernel, dim3((unsigned)grid, (unsigned)((rows + per_cta - 1) / per_cta)), dim3(kPagedThreads), 0, st, a, row_tile, shares); };
     if (shares > 8 * items) go(paged_join_kernel<T, HD, 4>, 1);
     else go(paged_join_kernel<T, HD, 1>, 4);
     return launch_check();

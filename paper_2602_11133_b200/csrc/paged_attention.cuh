@@ -238,6 +238,16 @@ __device__ __forceinline__ void paged_describe(const PagedArgs& a, const PagedRa
     else if (parts > 0) a.desc[share] = make_int4(b, item, parts, share);
 }
 
+// What a CTA of the second kernel joins, and whether there is anything: by item, a descriptor that nobody has written (its CTA gave up on a wait)
+// holds whatever the workspace held, so the item follows from the CTA alone, and parts that are not all in the workspace are left alone.
+struct PagedJoin {
+    int b, item, parts, share;
+};
+__host__ __device__ __forceinline__ bool paged_join_of(int4 d, bool by_item, int cta, int per_b, int shares, PagedJoin& j) {
+    j = by_item ? PagedJoin{cta / per_b, cta % per_b, d.z, d.w} : PagedJoin{d.x, d.y, d.z, d.w};
+    return j.parts > 0 && j.share >= 0 && j.share < shares && j.parts <= shares - j.share;
+}
+
 template <int HD>
 struct PagedSmem {
     static constexpr int TILE_BYTES = kPagedTile * HD * 2;                       // K or V of one stage
@@ -540,7 +550,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_attention_kernel(const Pa
 // Joins the parts of the items that several CTAs worked on.  blockIdx.x: the descriptor; WPR warps share a row, a part of the parts each, a
 // lane HD / 32 columns.
 template <typename T, int HD, int WPR>
-__global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedArgs a, int MT) {
+__global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedArgs a, int MT, int shares) {
     grid_launch_dependents();
     grid_dependency_wait();
     constexpr int E = HD / 32;
@@ -548,16 +558,16 @@ __global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedAr
     __shared__ float2 sml[4];
     const int R = a.T * a.group, RT = (R + MT - 1) / MT;
     if (a.by_item && paged_len(a, blockIdx.x / (a.nkv * RT)) <= 0) return;      // nobody had this item
-    const int4 d = a.desc[blockIdx.x];
-    if (d.z == 0) return;
+    PagedJoin d;
+    if (!paged_join_of(a.desc[blockIdx.x], a.by_item, blockIdx.x, a.nkv * RT, shares, d)) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int head = d.y / RT, row0 = (d.y - head * RT) * MT;
+    const int head = d.item / RT, row0 = (d.item - head * RT) * MT;
     const int r = blockIdx.y * (4 / WPR) + warp / WPR;
     if (r >= min(MT, R - row0)) return;                                 // (with WPR = 4 all of the CTA's warps have this row)
     float m = -INFINITY, l = 0.f, o[E] = {};
 #pragma unroll 4
-    for (int f = warp % WPR; f < d.z; f += WPR) {
-        const int64_t at = (f == 0 ? (int64_t)d.w * 2 + 1 : (int64_t)(d.w + f) * 2) * MT + r;
+    for (int f = warp % WPR; f < d.parts; f += WPR) {
+        const int64_t at = (f == 0 ? (int64_t)d.share * 2 + 1 : (int64_t)(d.share + f) * 2) * MT + r;
         const float2 p = a.partial_ml[at];
         float x[E];
 #pragma unroll
@@ -591,10 +601,10 @@ __global__ void __launch_bounds__(kPagedThreads) paged_join_kernel(const PagedAr
     }
     const float inv = 1.f / l;
     const int rr = row0 + r, t = rr / a.group, gq = rr - t * a.group;
-    T* out = (T*)a.out + d.x * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + lane * E;
+    T* out = (T*)a.out + d.b * a.o_b + (int64_t)t * a.o_t + (int64_t)(head * a.group + gq) * a.o_h + lane * E;
 #pragma unroll
     for (int e = 0; e < E; e += 2) *reinterpret_cast<typename Pack2<T>::type*>(out + e) = Pack2<T>::down(o[e] * inv, o[e + 1] * inv);
-    if (lane == 0 && a.lse) a.lse[((int64_t)d.x * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(l)) * 0.69314718055994531f;
+    if (lane == 0 && a.lse) a.lse[((int64_t)d.b * a.T + t) * a.nq + head * a.group + gq] = (m + log2f(l)) * 0.69314718055994531f;
 }
 
 }  // namespace jot

@@ -111,3 +111,18 @@ def test_a_scale_of_zero_gives_the_mean_of_the_values(jot, T):
             tol = torch.finfo(dtype).eps / 2 * (v.mean(0).abs() + v.abs().mean(0)) + 2.0 ** -18 * v.abs().mean(0)
             assert ((out - v.mean(0)).abs() <= tol).all()
             assert ((lse.double() - math.log(n)).abs() <= 2.0 ** -20 + 2.0 ** -22 * math.log(n)).all()
+
+
+# ---------------------------------------------------------------------------------------------- workspace
+@pytest.mark.parametrize("T", ROWS)
+@pytest.mark.parametrize("lens", [[20011], [1, 9000, 0, 700, -1, 5], [300] * 200])
+def test_what_a_workspace_holds_before_does_not_matter(jot, T, lens):
+    pages, table = spread(jot, 29, lens, 1, 16, 64, BF16)
+    q = normal(31, (len(lens), T, 1, 64), BF16)
+    ws = torch.empty(jot.paged_attention_workspace_bytes(T, 1, 1, 64), dtype=torch.uint8, device="cuda")
+    outs = []
+    for fill in (0, 0xff, 0x7f, 1):
+        ws.fill_(fill)
+        out, lse = check_attention(jot, q, pages, table, lens, workspace=ws)
+        outs.append((out.clone(), lse.clone()))
+    assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(o, outs[0]))
