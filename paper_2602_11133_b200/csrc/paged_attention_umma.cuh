@@ -272,9 +272,9 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
                 }
                 if (ok) more = w.next(a, per_b, KEYS);
             }
-            // somebody gave up: what is on its way must land before this CTA's shared memory is another's
+            // what is on its way must land before this CTA's shared memory is another's, also where somebody else has given up on using it
 #pragma unroll
-            for (int i = 0; !ok && i < RING; ++i) {
+            for (int i = 0; i < RING; ++i) {
                 const int st = (TWO ? 0 : s * RING) + i;
                 const uint32_t nk = (keys_sent + RING - 1 - i) / RING, nv = (values_sent + RING - 1 - i) / RING;
                 if (nk > 0) mbar_wait(&k_full[st], (nk - 1) & 1, &drain_flag);
@@ -440,10 +440,9 @@ paged_attention_umma_kernel(const PagedArgs a, const __grid_constant__ CUtensorM
             base += w.cnt;
             if (ok) more = w.next(a, per_b, KEYS);
         }
-        // the last arrival the tensor pipe owes this CTA's barriers; where somebody gave up, the end of the products under way
-        if (ok) {
-            wait_all(&v_empty[(TWO ? 0 : s * RING) + (base - 1) % RING], (base - 1) / RING & 1);
-        } else {
+        // the last arrival the tensor pipe owes this CTA's barriers; where somebody gave up, meanwhile too, the end of the products under way
+        if (ok) ok = wait_all(&v_empty[(TWO ? 0 : s * RING) + (base - 1) % RING], (base - 1) / RING & 1);
+        if (!ok) {
             if (elected) umma_commit(&drain[s]);
             __syncwarp();
             mbar_wait(&drain[s], 0, &drain_flag);

@@ -97,3 +97,14 @@ def test_descriptors_that_nobody_wrote_lead_nowhere(tmp_path):
     # and the second kernel asks it before anything else of the descriptor is used
     kernel = sources()["paged_attention.cuh"].split("paged_join_kernel(")[1]
     assert kernel.count("a.desc[") == 1 and "if (!paged_join_of(a.desc[blockIdx.x], a.by_item, blockIdx.x, a.nkv * RT, shares, d)) return;" in kernel
+
+
+def test_no_cta_leaves_with_copies_or_products_under_way():
+    """A role that is through with its work cannot know that another one gives up after it: the copies it has sent are waited for, and the
+    products it has issued, whether or not it has given up itself (what would happen otherwise cannot be tried out)."""
+    text = sources()["paged_attention_umma.cuh"]
+    producers = text.split("// ================================ producers")[1].split("// ================================ products")[0]
+    drain = producers.split("for (int i = 0; i < RING; ++i) {")[1].split("\n            }")[0]
+    assert "mbar_wait(&k_full[st], (nk - 1) & 1, &drain_flag)" in drain and "mbar_wait(&v_full[st], (nv - 1) & 1, &drain_flag)" in drain
+    end = text.split("// ================================ products")[1].split("// ================================ softmax")[0].split("tails += has_tail;")[1]
+    assert "if (ok) ok = wait_all(&v_empty[" in end and "if (!ok) {" in end and "umma_commit(&drain[s]);" in end and "mbar_wait(&drain[s], 0, &drain_flag);" in end
