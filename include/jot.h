@@ -224,7 +224,8 @@ int jot_denoise_step_cached(jot_model* m, const int32_t* d_tokens, int B, int L,
  * read by every pass and may change between them; a page that lies outside the pages is reported as JOT_ERR_ARG.  Pages of positions
  * that a pass writes (refresh: all; otherwise the block's) must belong to one sequence of the batch only.  The struct is copied; pages,
  * table and workspace (device, 256-byte aligned, jot_kv_pages_workspace_bytes() long) are borrowed until detached or the model is freed.
- * Writes a table into the workspace (synchronous). */
+ * Writes a table into the workspace: synchronous, on no stream of the caller's, so that work which still uses the workspace's memory has to
+ * be finished before. */
 struct jot_kv_pages;
 size_t jot_kv_pages_workspace_bytes(const jot_model_config* cfg, int max_batch, int max_seq);
 int jot_attach_kv_pages(jot_model* m, const struct jot_kv_pages* pages, const int32_t* d_page_table, int64_t table_stride,

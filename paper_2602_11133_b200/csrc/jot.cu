@@ -1246,6 +1246,7 @@ int jot_attach_kv_pages(jot_model* m, const jot_kv_pages* pages, const int32_t* 
     for (int j = 0; j < c.head_dim / 2; ++j) freq[j] = (float)std::pow((double)c.rope_theta, -2.0 * j / c.head_dim);
     m->inv_freq = (float*)(base + l.inv_freq);
     JOT_CUDA(cudaMemcpy(m->inv_freq, freq, (size_t)c.head_dim / 2 * 4, cudaMemcpyHostToDevice));
+    JOT_CUDA(cudaStreamSynchronize(cudaStreamLegacy));             // (a copy from pageable memory may return before it has arrived)
     m->page_positions = (int32_t*)(base + l.positions);
     m->page_slots = (int32_t*)(base + l.slots);
     m->page_lens = (int32_t*)(base + l.lens);

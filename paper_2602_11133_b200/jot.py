@@ -293,6 +293,7 @@ class Model:
             raise ValueError(f"attach_kv_pages: the table has {page_table.shape[0]} rows, the model takes {self.max_batch} sequences")
         nbytes = _lib().jot_kv_pages_workspace_bytes(C.byref(self.cfg), self.max_batch, self.max_seq)
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        torch.cuda.current_stream(dev).synchronize()         # kernels queued on it may still write what is the workspace's memory now
         _check(_lib().jot_attach_kv_pages(self.handle, pages._packed, page_table.data_ptr(), page_table.stride(0), page_table.shape[1],
                                           workspace.data_ptr(), nbytes), "jot_attach_kv_pages")
         self.kv_cache = (pages, page_table, workspace)       # keep them alive

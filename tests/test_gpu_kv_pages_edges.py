@@ -55,3 +55,21 @@ def busy_block(nbytes):
     torch.cuda._sleep(400_000_000)                                 # some 0.2 s
     block.fill_(0x55)
     return block.data_ptr()
+
+
+def test_pages_attached_on_a_busy_stream(jot):
+    """The workspace of attached pages may be memory that kernels queued on the stream have yet to write."""
+    import ctypes as C
+    g, model, canvas, lo, hi = small(jot)
+    pages, table = in_pages(jot, model, g, 2, canvas.shape[1], 16)
+    n = g.head_dim // 2
+    want = model.kv_cache[2][:4 * n].view(torch.float32).clone()
+    nbytes = jot._lib().jot_kv_pages_workspace_bytes(C.byref(model.cfg), 2, canvas.shape[1])
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        at = busy_block(nbytes)
+        model.attach_kv_pages(pages, table)
+        assert model.kv_cache[2].data_ptr() == at                  # the block, or this test shows nothing
+        torch.cuda.synchronize()
+        assert torch.equal(model.kv_cache[2][:4 * n].view(torch.float32), want)
+    model.close()
