@@ -150,7 +150,8 @@ typedef struct jot_model jot_model; /* opaque; host-side object owned by the lib
 size_t jot_workspace_bytes(const jot_model_config* cfg, int max_batch, int max_seq);
 
 /* Create a model over borrowed weights and a caller-owned workspace (device, 1024-byte aligned, at
- * least jot_workspace_bytes()).  Writes tables into the workspace (synchronous).  The workspace must
+ * least jot_workspace_bytes()).  Writes tables into the workspace: synchronous, on no stream of the
+ * caller's, so that work which still uses that memory has to be finished before.  The workspace must
  * stay alive and untouched by the caller until jot_free_model.  One model must not be used from two
  * streams at once. */
 int jot_init_model(const jot_model_config* cfg, const jot_weights* weights, int max_batch, int max_seq,

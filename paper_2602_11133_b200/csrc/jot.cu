@@ -1106,6 +1106,7 @@ int jot_init_model(const jot_model_config* cfg, const jot_weights* w, int max_ba
     if (e == cudaSuccess) e = cudaMemset(m->hsel, 0, (size_t)m->R_cap * d * 2);
     if (e == cudaSuccess) e = cudaMemset(m->rows, 0, (size_t)m->R_cap * 4);
     if (e == cudaSuccess) e = cudaMemset(m->rows_out, 0, (size_t)m->R_cap * 4);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);       // steps may run on streams that do not wait for this one
     for (int i = 0; i < 2 && e == cudaSuccess; ++i) e = cudaEventCreateWithFlags(&m->step_done[i], cudaEventDisableTiming);
     if (e == cudaSuccess) e = cudaHostAlloc((void**)&m->h_pinned, 64 + (size_t)max_batch * sizeof(SeqState), cudaHostAllocDefault);
     if (e != cudaSuccess) {

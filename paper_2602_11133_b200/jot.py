@@ -256,6 +256,7 @@ class Model:
                      _ptr(weights["final_norm"], torch.bfloat16, "final_norm"),
                      *[C.cast(a, C.POINTER(C.c_void_p)) for a in self._arrays])
         handle = C.c_void_p()
+        torch.cuda.current_stream(dev).synchronize()         # kernels queued on it may still write what is the workspace's memory now
         _check(lib.jot_init_model(C.byref(self.cfg), C.byref(w), max_batch, max_seq, base, nbytes, C.byref(handle)),
                "jot_init_model")
         self.handle = handle

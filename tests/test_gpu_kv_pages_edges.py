@@ -73,3 +73,18 @@ def test_pages_attached_on_a_busy_stream(jot):
         torch.cuda.synchronize()
         assert torch.equal(model.kv_cache[2][:4 * n].view(torch.float32), want)
     model.close()
+
+
+def test_a_model_made_on_a_busy_stream(jot):
+    g, model, canvas, lo, hi = small(jot)
+    want = model.denoise_step(canvas, lo, hi).sumexp.clone()
+    nbytes, w = model.workspace.numel(), model.weights
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        at = busy_block(nbytes)
+        other = jot.Model(g, w, 2, canvas.shape[1])
+        assert other.workspace.data_ptr() == at
+        torch.cuda.synchronize()
+        assert int(control(other)) == 0                            # (before any kernel works with what the model holds)
+        assert torch.equal(other.denoise_step(canvas, lo, hi).sumexp, want)
+    model.close(), other.close()
