@@ -496,6 +496,7 @@ struct jot_model {
     std::vector<CUtensorMap> kv_tm_qkv3, kv_tm_vt;
     int kv_map_B = -1, kv_map_L = -1;       // geometry the per-layer maps were encoded for
     int kv_valid_B = -1, kv_valid_L = -1;   // geometry of the last refresh (block passes need one)
+    bool kv_unread = false;                 // a refresh has been enqueued whose status nobody has read yet
     // the same cache in pages instead (caller's memory too): keys and values only, wherever the page table says
     bool paged = false;
     jot_kv_pages pages;
@@ -695,6 +696,7 @@ PagesLayout pages_layout(const jot_model_config* c, int max_batch, int max_seq) 
 struct FwdSpan {
     int Lr, pos0;
     bool use_cache;
+    bool refresh;                           // the pass fills the cache anew: whatever comes of it, what was there before is gone
 };
 
 // A layer between its projections, over pages: the QKV rows of the pass rotated in place, keys and values into the pages, attention of the
@@ -722,6 +724,7 @@ int forward_body(jot_model* m, const int32_t* d_tokens, int B, int L, cudaStream
     const jot_model_config& c = m->cfg;
     const int Lr = span ? span->Lr : L, pos0 = span ? span->pos0 : 0;
     const bool paged = span && span->use_cache && m->paged, cached = span && span->use_cache && !m->paged;
+    if (span && span->refresh) m->kv_valid_B = m->kv_valid_L = -1;
     const int M = B * Lr, d = c.d_model, hd = c.head_dim, nq = c.n_q_heads, nkv = c.n_kv_heads;
     const int qkv_cols = (nq + 2 * nkv) * hd;
     const int Lp = (int)align_up((size_t)L, 8);
@@ -934,12 +937,18 @@ int check_step_args(const jot_model* m, const void* tokens, int B, int L, int bl
 bool status_of_input(int32_t w) { return w == kStatusBadToken || w == kStatusBadIndex; }
 int status_code(int32_t w) { return w == 0 ? JOT_OK : (status_of_input(w) ? JOT_ERR_ARG : JOT_ERR_TIMEOUT); }
 
+// A status word that has been read, as a call's result.
+int take_status(jot_model* m, int32_t w, cudaStream_t st) {
+    if (w != 0 && m->kv_unread) m->kv_valid_B = m->kv_valid_L = -1;           // it may be the refresh's: the cache holds a mixture then
+    m->kv_unread = false;
+    if (status_of_input(w)) JOT_CUDA(cudaMemsetAsync(m->ctrl, 0, 4, st));     // the caller can fix its input and go on
+    return status_code(w);
+}
+
 int read_status(jot_model* m, cudaStream_t st) {
     JOT_CUDA(cudaMemcpyAsync(m->h_pinned, m->ctrl, 4, cudaMemcpyDeviceToHost, st));
     JOT_CUDA(cudaStreamSynchronize(st));
-    const int32_t w = m->h_pinned[0];
-    if (status_of_input(w)) JOT_CUDA(cudaMemsetAsync(m->ctrl, 0, 4, st));     // the caller can fix its input and go on
-    return status_code(w);
+    return take_status(m, m->h_pinned[0], st);
 }
 
 int launch_accept(const AcceptArgs& a, cudaStream_t st, const AcceptParamsInline* inl = nullptr) {
@@ -1268,10 +1277,10 @@ int jot_denoise_step_cached(jot_model* m, const int32_t* d_tokens, int B, int L,
     if (!m || !(m->kv_base || m->paged)) return JOT_ERR_ARG;
     if (blk_lo >= blk_hi) return JOT_ERR_ARG;
     if (!refresh && (m->kv_valid_B != B || m->kv_valid_L != L)) return JOT_ERR_ARG;     // nothing cached for this canvas
-    const FwdSpan span = refresh ? FwdSpan{L, 0, true} : FwdSpan{blk_hi - blk_lo, blk_lo, true};
+    const FwdSpan span = refresh ? FwdSpan{L, 0, true, true} : FwdSpan{blk_hi - blk_lo, blk_lo, true, false};
     const int rc = denoise_step_impl(m, d_tokens, B, L, blk_lo, blk_hi, exclude_mask_token, d_bump_id, d_bump_val, d_top1,
                                      d_top2, d_sumexp, d_argmax, sampling, d_sampled, stream, &span);
-    if (rc == JOT_OK && refresh) { m->kv_valid_B = B; m->kv_valid_L = L; }
+    if (rc == JOT_OK && refresh) { m->kv_valid_B = B; m->kv_valid_L = L; m->kv_unread = !m->sync_steps; }
     return rc;
 }
 
@@ -1372,7 +1381,7 @@ int jot_generate(jot_model* m, const jot_params* params, int per_seq_params, con
             const int lo = P + blk * Lb, hi = lo + Lb;
             for (int s = 0; s < Tb; ++s) {
                 JOT_CUDA(cudaMemsetAsync(m->ctrl + 2, 0, 4, st));
-                const FwdSpan span = (s == 0) ? FwdSpan{L, 0, true} : FwdSpan{Lb, lo, true};
+                const FwdSpan span = (s == 0) ? FwdSpan{L, 0, true, true} : FwdSpan{Lb, lo, true, false};
                 JOT_TRY(forward_to_head(m, m->canvas, B, L, st, nullptr, &span, ActiveRows{lo, hi, nullptr, 0, 0, 0, B * Lb}));
                 JOT_TRY(lm_head_from_hsel(m, gen->exclude_mask_token, d_bump_id, d_bump_val, m->g_top1, m->g_top2,
                                           m->g_sumexp, m->g_argmax, B * Lb, st, &hs));
@@ -1394,16 +1403,11 @@ int jot_generate(jot_model* m, const jot_params* params, int per_seq_params, con
                 }
                 JOT_CUDA(cudaMemcpyAsync(m->h_pinned, m->ctrl, 16, cudaMemcpyDeviceToHost, st));
                 JOT_CUDA(cudaStreamSynchronize(st));
-                if (m->h_pinned[0]) {
-                    const int32_t w0 = m->h_pinned[0];
-                    if (status_of_input(w0)) cudaMemsetAsync(m->ctrl, 0, 4, st);
-                    return status_code(w0);
-                }
+                if (m->h_pinned[0]) return take_status(m, m->h_pinned[0], st);
                 ++n_passes;
                 if (m->h_pinned[2] == 0) break;              // no sequence has a masked position left in this block
             }
         }
-        m->kv_valid_B = m->kv_valid_L = -1;                  // the cache belongs to a canvas that is finished
         JOT_CUDA(cudaMemcpyAsync(d_out_tokens, m->canvas, (size_t)B * L * 4, cudaMemcpyDeviceToDevice, st));
         SeqState* hstate = reinterpret_cast<SeqState*>(m->h_pinned + 16);
         JOT_CUDA(cudaMemcpyAsync(hstate, m->state, (size_t)B * sizeof(SeqState), cudaMemcpyDeviceToHost, st));

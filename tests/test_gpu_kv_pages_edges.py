@@ -49,6 +49,73 @@ def test_a_bad_page_does_not_take_an_expired_wait_off_the_record(jot):
     model.close()
 
 
+@pytest.mark.parametrize("paged", [True, False])
+@pytest.mark.parametrize("sync", [True, False])
+def test_a_refresh_that_failed_leaves_no_canvas(jot, paged, sync):
+    """Blocks are attended over what a refresh left; one that was told of a bad page or a bad token left a mixture."""
+    g, model, canvas, lo, hi = small(jot)
+    if paged:
+        _, table = in_pages(jot, model, g, 2, canvas.shape[1], 16)
+    else:
+        model.attach_kv_cache()
+    block = lambda: model.denoise_step_cached(canvas, lo, hi, refresh=False)
+    model.set_sync(sync)
+
+    def failing_refresh():
+        bad = canvas.clone()
+        if paged:
+            good = table.clone()
+            table[1, 1] = 10 ** 6
+        else:
+            bad[0, 0] = g.vocab + 3
+        if sync:
+            refused(jot, -1, lambda: model.denoise_step_cached(bad, lo, hi, refresh=True))
+        else:
+            model.denoise_step_cached(bad, lo, hi, refresh=True)
+            refused(jot, -1, model.read_status)
+        if paged:
+            table.copy_(good)
+
+    failing_refresh()
+    refused(jot, -1, block)
+    model.denoise_step_cached(canvas, lo, hi, refresh=True)
+    want = block().sumexp.clone()
+    failing_refresh()
+    refused(jot, -1, block)                                        # (the refresh before the failing one was of the same shape)
+    model.denoise_step_cached(canvas, lo, hi, refresh=True)
+    assert torch.equal(block().sumexp, want)
+    # calls that are refused before anything is enqueued touch no cache
+    with pytest.raises(jot.JotError):
+        model.denoise_step_cached(canvas, lo, canvas.shape[1] + 1, refresh=True)
+    assert torch.equal(block().sumexp, want)
+    # a block that fails leaves the rest of the canvas alone: it can be run again
+    bad = canvas.clone()
+    bad[0, lo] = g.vocab + 3
+    if sync:
+        refused(jot, -1, lambda: model.denoise_step_cached(bad, lo, hi, refresh=False))
+    else:
+        model.read_status()
+        model.denoise_step_cached(bad, lo, hi, refresh=False)
+        refused(jot, -1, model.read_status)
+    assert torch.equal(block().sumexp, want)
+    model.set_sync(True)
+    model.read_status()
+    model.close()
+
+
+def test_a_generation_that_failed_leaves_no_canvas(jot):
+    g, model, canvas, lo, hi = small(jot)
+    _, table = in_pages(jot, model, g, 2, canvas.shape[1], 16)
+    good = table.clone()
+    prompt = inputs.prompt(3, 2, 40, g.vocab, g.mask_id).cuda()
+    model.denoise_step_cached(canvas, lo, hi, refresh=True)
+    table[1, 1] = -1
+    refused(jot, -1, lambda: model.generate(prompt, 56, 14, jot.Params(), block_len=28, kv_cache=True))
+    table.copy_(good)
+    refused(jot, -1, lambda: model.denoise_step_cached(canvas, lo, hi, refresh=False))
+    model.close()
+
+
 def busy_block(nbytes):
     """On the current stream: a block of memory that a queued kernel will still write when the block is already free again."""
     block = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
