@@ -1350,10 +1350,7 @@ int jot_generate(jot_model* m, const jot_params* params, int per_seq_params, con
     auto outcome = [&](int slot, bool* finished) -> int {      // wait for a step's control words
         JOT_CUDA(cudaEventSynchronize(m->step_done[slot]));
         const int32_t* w = m->h_pinned + 4 * slot;
-        if (w[0]) {
-            if (w[0] == kStatusBadToken) cudaMemsetAsync(m->ctrl, 0, 4, st);
-            return status_code(w[0]);
-        }
+        if (w[0]) return take_status(m, w[0], st);
         *finished = w[2] == 0;
         if (!*finished) B_act = w[2];
         return JOT_OK;

@@ -49,6 +49,18 @@ def test_a_bad_page_does_not_take_an_expired_wait_off_the_record(jot):
     model.close()
 
 
+def test_a_bad_page_of_an_earlier_pass_is_reported_once_by_generate(jot):
+    g, model, canvas, lo, hi = small(jot)
+    _, table = in_pages(jot, model, g, 2, canvas.shape[1], 16)
+    prompt = inputs.prompt(3, 2, 40, g.vocab, g.mask_id).cuda()
+    model.set_sync(False)
+    table[1, 0] = 10 ** 6
+    model.denoise_step_cached(canvas, lo, hi, refresh=True)
+    refused(jot, -1, lambda: model.generate(prompt, 56, 14, jot.Params(), block_len=28))
+    model.generate(prompt, 56, 14, jot.Params(), block_len=28)
+    model.close()
+
+
 @pytest.mark.parametrize("paged", [True, False])
 @pytest.mark.parametrize("sync", [True, False])
 def test_a_refresh_that_failed_leaves_no_canvas(jot, paged, sync):
