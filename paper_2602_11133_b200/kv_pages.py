@@ -7,6 +7,7 @@ slots as plain lists for tensors.  Pages can be shared: a fork costs no page unt
 from __future__ import annotations
 
 import heapq
+import operator
 from typing import Dict, Hashable, Iterable, List, Sequence, Tuple
 
 Copies = Tuple[List[int], List[int]]        # pages to read, pages to write
@@ -18,6 +19,7 @@ class OutOfPages(RuntimeError):
 
 class PagePool:
     def __init__(self, n_pages: int, page_size: int):
+        n_pages, page_size = operator.index(n_pages), operator.index(page_size)
         if n_pages <= 0 or page_size <= 0:
             raise ValueError("PagePool: n_pages and page_size must be positive")
         self.n_pages, self.page_size = n_pages, page_size
@@ -57,6 +59,7 @@ class PagePool:
     # ---- sequences ----------------------------------------------------------------------------------------------
     def add(self, seq: Hashable, length: int) -> None:
         """A new sequence of `length` positions in pages of its own."""
+        length = operator.index(length)
         if seq in self._pages:
             raise ValueError(f"PagePool: sequence {seq!r} is there already")
         self._pages[seq], self._length[seq] = [], 0
@@ -69,6 +72,7 @@ class PagePool:
     def resize(self, seq: Hashable, length: int) -> None:
         """Pages for `length` positions: new ones behind the last, or the last ones given back.  (Positions that come into a
         page another sequence has, too, need own() before they are written.)"""
+        length = operator.index(length)
         if length < 0:
             raise ValueError("PagePool: negative length")
         pages = self._pages[seq]

@@ -7,6 +7,7 @@ import subprocess
 import pytest
 
 from paper_2602_11133_b200 import build as jot_build
+from paper_2602_11133_b200.kv_pages import PagePool
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2602_11133_b200", "csrc")
@@ -108,3 +109,18 @@ def test_no_cta_leaves_with_copies_or_products_under_way():
     assert "mbar_wait(&k_full[st], (nk - 1) & 1, &drain_flag)" in drain and "mbar_wait(&v_full[st], (nv - 1) & 1, &drain_flag)" in drain
     end = text.split("// ================================ products")[1].split("// ================================ softmax")[0].split("tails += has_tail;")[1]
     assert "if (ok) ok = wait_all(&v_empty[" in end and "if (!ok) {" in end and "umma_commit(&drain[s]);" in end and "mbar_wait(&drain[s], 0, &drain_flag);" in end
+
+
+def test_lengths_that_are_no_integers_change_nothing_in_a_pool():
+    pool = PagePool(4, 16)
+    for call in (lambda: pool.add("a", 17.0), lambda: pool.add("a", "17"), lambda: pool.add("a", None)):
+        with pytest.raises(TypeError):
+            call()
+        with pytest.raises(KeyError):
+            pool.length("a")
+    pool.add("a", 17)                          # the name is free
+    with pytest.raises(TypeError):
+        pool.resize("a", 16.5)                 # as many pages as before: it would have become a length
+    assert pool.length("a") == 17 and pool.free_pages == 2
+    with pytest.raises(TypeError):
+        PagePool(4, 2.5)
