@@ -113,6 +113,53 @@ def test_a_scale_of_zero_gives_the_mean_of_the_values(jot, T):
             assert ((lse.double() - math.log(n)).abs() <= 2.0 ** -20 + 2.0 ** -22 * math.log(n)).all()
 
 
+@pytest.mark.parametrize("page", PAGES)
+@pytest.mark.parametrize("T", ROWS)
+def test_infinite_and_nan_scores_in_every_form(jot, T, page):
+    """A NaN query, an infinite one and an infinite key element reach the rows whose scores they are, and no other."""
+    n, hd = 333, 64
+    for dtype in (BF16, FP16):
+        pages, table = spread(jot, 11, [n, n], 1, page, hd, dtype)
+        args = table.cuda(), int32([n, n])
+        q = normal(13, (2, T, 1, hd), dtype)
+        q[..., 0] = torch.where(q[..., 0] >= 0, 1.0, -1.0).to(dtype)
+        plain = jot.paged_attention(q, pages, *args)
+        # NaN and infinite queries: their rows are NaN (an infinite query meets keys of either sign), the others keep their bits
+        bad = q.clone()
+        bad[0, T // 2, 0, 3], bad[1, 0, 0, 0] = math.nan, math.inf
+        out = jot.paged_attention(bad, pages, *args)
+        hit = torch.zeros(2, T, dtype=torch.bool, device="cuda")
+        hit[0, T // 2] = hit[1, 0] = True
+        assert out[hit].isnan().all() and torch.equal(out[~hit], plain[~hit])
+        # an infinite key element: rows with a positive query element there have a score of infinity, whose softmax is no number; for the others
+        # the key does not count: as if it scored far below all others
+        k, v = (t[0][table[0, :(n + page - 1) // page].long().cuda(), 0].reshape(-1, hd)[:n].double() for t in (pages.k, pages.v))
+        for j in (0, 130, n - 1):
+            saved = pages.k[0, table[0, j // page], 0, j % page, 0].clone()
+            pages.k[0, table[0, j // page], 0, j % page, 0] = math.inf
+            lse = torch.empty(2, T, 1, device="cuda")
+            out = jot.paged_attention(q, pages, *args, lse=lse)
+            up = q[0, :, 0, 0] > 0
+            assert out[0][up].isnan().all() and not lse[0][up].isfinite().any()
+            s = q[0, :, 0].double() @ k.T * hd ** -0.5
+            s[:, j] = -math.inf
+            p = torch.softmax(s, -1)
+            eps = torch.finfo(dtype).eps
+            tol = eps / 2 * ((p @ v).abs() + p @ v.abs()) + 2.0 ** -14 * (p @ v.abs()) + 2.0 ** -24
+            assert ((out[0, :, 0].double() - p @ v).abs() <= tol)[~up].all()
+            assert torch.equal(out[1], plain[1])
+            pages.k[0, table[0, j // page], 0, j % page, 0] = saved
+        # scores of minus infinity only: nothing to weigh, and the logarithm of nothing
+        pages.k[0, :, 0, :, 0] = pages.k[0, :, 0, :, 0].abs().clamp(min=0.5)
+        bad = q.clone()
+        bad[0, 1, 0, 0] = -math.inf
+        lse = torch.empty(2, T, 1, device="cuda")
+        out, again = jot.paged_attention(bad, pages, *args, lse=lse), jot.paged_attention(q, pages, *args)
+        hit = torch.zeros(2, T, dtype=torch.bool, device="cuda")
+        hit[0, 1] = True
+        assert out[hit].isnan().all() and (lse[hit] == -math.inf).all() and torch.equal(out[~hit], again[~hit])
+
+
 # ---------------------------------------------------------------------------------------------- workspace
 @pytest.mark.parametrize("T", ROWS)
 @pytest.mark.parametrize("lens", [[20011], [1, 9000, 0, 700, -1, 5], [300] * 200])
