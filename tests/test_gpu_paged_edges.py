@@ -160,6 +160,52 @@ def test_infinite_and_nan_scores_in_every_form(jot, T, page):
         assert out[hit].isnan().all() and (lse[hit] == -math.inf).all() and torch.equal(out[~hit], again[~hit])
 
 
+# ---------------------------------------------------------------------------------------------- pages and lengths outside
+@pytest.mark.parametrize("page", PAGES + [256])
+@pytest.mark.parametrize("T", ROWS)
+def test_pages_outside_the_pool_read_as_zeros_in_every_form(jot, T, page):
+    lens = [700, 40]
+    for hd in (64, 128):
+        pages, table = spread(jot, 45, lens, 2, page, hd, BF16)
+        used = set(table[table >= 0].tolist())
+        blank = next(p for p in range(pages.n_pages) if p not in used)
+        pages.k[0, blank] = pages.v[0, blank] = 0
+        q = normal(8, (2, T, 2, hd), BF16)
+        dl = int32(lens)
+        for at in (0, 1, (lens[0] - 1) // page):
+            t = table.clone()
+            t[0, at] = blank
+            want, _ = check_attention(jot, q, pages, t, lens)
+            for bad in (-1, pages.n_pages, 2 ** 31 - 1, -2 ** 31):
+                t[0, at] = bad
+                status = int32([0])
+                out = jot.paged_attention(q, pages, t.cuda(), dl, status=status)
+                assert int(status) == jot.STATUS_BAD_INDEX and torch.equal(out, want)
+        # a length beyond the table's row counts up to its end
+        status = int32([0])
+        t = table[:, :2].cuda()
+        out = jot.paged_attention(q, pages, t, int32([2 ** 31 - 1, 40 if page > 20 else 2 * page]), status=status)
+        assert int(status) == jot.STATUS_BAD_INDEX
+        assert torch.equal(out, jot.paged_attention(q, pages, t, int32([2 * page, 40 if page > 20 else 2 * page])))
+
+
+@pytest.mark.parametrize("T", ROWS)
+def test_pages_that_lie_backwards(jot, T):
+    """A page stride below zero (the library's interface takes it): the pool from its other end."""
+    n, hd, page = 500, 64, 16
+    pages, table = spread(jot, 17, [n], 2, page, hd, BF16)
+    q = normal(19, (1, T, 4, hd), BF16)
+    stride, last = pages.k.stride(1), pages.n_pages - 1
+    turned = jot.KVPages(pages.k.flip(1).contiguous(), pages.v.flip(1).contiguous())       # what the pool is, seen from there
+    turned._packed = jot._pack_pages(pages.k[0, last].data_ptr(), pages.v[0, last].data_ptr(), pages.k.stride(0), pages.v.stride(0), -stride, -stride, 1,
+                                     pages.n_pages, 2, page, hd, 0)
+    check_attention(jot, q, turned, torch.where(table >= 0, last - table, table), [n])
+    x, slots = normal(23, (3, 4, hd), BF16), int32([0, 5 * page + 3, last * page + 1])
+    jot.kv_write(turned, x[:, :2], x[:, 2:], slots)
+    for r, s in enumerate(slots.tolist()):
+        assert torch.equal(pages.k[0, last - s // page, :, s % page], x[r, :2]) and torch.equal(pages.v[0, last - s // page, :, s % page], x[r, 2:])
+
+
 # ---------------------------------------------------------------------------------------------- workspace
 @pytest.mark.parametrize("T", ROWS)
 @pytest.mark.parametrize("lens", [[20011], [1, 9000, 0, 700, -1, 5], [300] * 200])
