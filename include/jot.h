@@ -413,7 +413,7 @@ int jot_kv_copy_pages(const jot_kv_pages* pages, int n, const int32_t* src, cons
  * h / (n_q_heads / n_kv_heads).  d_lse (nullable, [B, T, n_q_heads] fp32): ln of the sum of exp(scale * q . k);
  * scale times log2(e) is finite (JOT_ERR_ARG otherwise).  A length of 0 gives zeros and -inf.  head_dim 64 or 128.  Fewer than 2^31 tiles of 64 keys over all sequences, heads and rows, were every
  * sequence as long as its table row allows.  Entries of a table row past its length are not read.  Tokens past a length within
- * a page may hold anything, NaN included.
+ * a page may hold anything, NaN included.  (An infinite value of a key that counts makes its column of the results infinite or NaN.)
  * d_workspace: at least jot_paged_attention_workspace_bytes() (0 on invalid arguments), 16-byte aligned, the call's own until it
  * has finished on the device: two calls (or two graphs) that may run at the same time need one each. */
 size_t jot_paged_attention_workspace_bytes(int T, int n_q_heads, int n_kv_heads, int head_dim);

@@ -105,7 +105,8 @@ PagedSpace paged_space(int row_tile, int head_dim) {
 // Items of a call: (sequence, key head, tile of rows).
 int64_t paged_items(const PagedArgs& a, int row_tile) { return (int64_t)a.B * a.nkv * ((a.T * a.group + row_tile - 1) / row_tile); }
 
-// The second kernel: four warps to a row where an item may be in many parts (few items on many CTAs), else a warp to a row.
+// The second kernel: four warps to a row where an item may be in many parts (few items on many CTAs), else a warp to a row.  One row over 20011 keys
+// 23 us with four and 50 with one, 224 rows over 8192 keys 22 and 36; 32 rows of 32 heads of 16 sequences 50 and 44, canvases of 704 rows 230 and 202.
 template <typename T, int HD>
 int launch_join(const PagedArgs& a, int shares, int row_tile, cudaStream_t st) {
     const int rows = std::min(row_tile, a.T * a.group);
@@ -197,7 +198,9 @@ int launch_paged_umma(const DeviceInfo* di, PagedArgs a, int64_t items, cudaStre
     const bool tma = paged_tma_pages(a.pages.page_size) && a.pages.k_page >= 0 && a.pages.v_page >= 0;
     const int64_t tiles = paged_tiles(a, tma ? paged_tma_keys(a.pages.page_size) : kUmmaPagedTile);
     constexpr int streams = ROWS == 256 ? 1 : 2;
-    // two tiles of rows take twice as long over a tile of keys: worth cutting unless a third of the SMs have items of their own
+    // Two tiles of rows take twice as long over a tile of keys: worth cutting unless a third of the SMs have items of their own.  224 rows over 512
+    // keys: one sequence 13.3 us cut and 15.4 whole, four 16.4 and 16.3, sixteen 23.1 and 17.8; canvases of 384 rows of 32 heads 26.5 and 15.3.  (Over
+    // 256 keys whole items are ahead for few sequences, too: 12.1 and 11.1 for one, 16.6 and 12.4 for eight.)
     a.whole = tiles <= 1 || (tiles <= kPagedWhole && (ROWS < 256 || 3 * items * a.B >= di->sms));
     const int grid = (int)std::min<int64_t>(paged_most(a, items, tiles), std::min(di->sms, kUmmaPagedMaxCtas));
     a.by_item = !a.whole && paged_items(a, ROWS) <= grid * streams;
@@ -283,6 +286,8 @@ int jot_head_norm_rope(const jot_heads* q, const jot_heads* k, const jot_rope* r
     if (k) a.k = heads_dev(k);
     a.positions = d_positions; a.inv_freq = rope->d_inv_freq; a.half = rope->rotary_dim / 2; a.magnitude = rope->magnitude; a.eps = eps;
     a.head_dim = head_dim; a.n_rows = n_rows; a.slots = d_slots; a.status = d_status;
+    // Several rows a CTA where there are many: 11264 rows of 64 heads 64 us, 79 at one a CTA, 6024 rows of 32 heads 23 and 34; from a quarter as many
+    // rows on it would cost: 512 rows of 64 heads 9.5 us, 7.0 at one.
     a.rows_per_cta = n_rows >= 16 * di->sms ? 4 : (n_rows >= 8 * di->sms ? 2 : 1);
     cudaStream_t st = (cudaStream_t)stream;
     const bool il = rope->interleaved != 0;
@@ -311,6 +316,8 @@ int jot_kv_write(const jot_kv_pages* pages, int layer, int n_rows, const void* d
     a.k_row = k_row_stride; a.k_head = k_head_stride; a.v_row = v_row_stride; a.v_head = v_head_stride;
     a.n_rows = n_rows; a.n_heads = pages->n_kv_heads; a.head_dim = pages->head_dim;
     a.pages = layer_pages(pages, layer); a.slots = d_slots; a.status = d_status;
+    // Several short rows a CTA, while every SM has eight: 40000 rows of 4 heads of 128 28 us, 43 at one a CTA; 11264 rows of 4 heads 10.9 and 13.6, of
+    // 32 heads (two a CTA) 57.9 and 56.2.
     const int per_row = a.n_heads * (a.head_dim / 8);
     a.rows_per_cta = std::max(1, std::min(n_rows / (8 * di->sms), 4 * kMoveThreads / per_row));
     launch_k(kv_write_kernel, dim3((unsigned)((n_rows + a.rows_per_cta - 1) / a.rows_per_cta)), dim3(kMoveThreads), 0, (cudaStream_t)stream, a);
@@ -335,6 +342,7 @@ int jot_kv_copy_pages(const jot_kv_pages* pages, int n, const int32_t* src, cons
                                                                                          INT32_MAX / 4 / a.n_layers)));
     for (int i = 0; i < n; i += step) {
         const int m = std::min(step, n - i);
+        // (few pairs are few bytes of arguments: five pages 8.4 us a call, 9.2 with room for 1024; on the device the same)
         if (m <= 16) JOT_TRY(launch_copy<16>(a, src + i, dst + i, m, st));
         else JOT_TRY(launch_copy<MOST>(a, src + i, dst + i, m, st));
     }

@@ -17,12 +17,13 @@
 // ahead), two CTAs an SM; its four warps have 16 keys of a stage each, and a maximum, a sum and an accumulator of their own until the
 // item ends.  16-byte chunk c of a row sits at position c ^ (row mod 8): eight rows of one chunk are on eight different banks for
 // ldmatrix.  Scores, statistics and accumulators are fp32; probabilities are rounded to the cache's type for the second product (the
-// sum is taken before the rounding).
+// sum is taken before the rounding: the rounding's errors average out over the keys, and fp16's smallest numbers are out of their way, kPagedLift).
 //
-// One row of 28 query over 4 key heads for four sequences of 40007 to 131072 keys (700 MB): 118-123 us, 5.7-6.0 TB/s, 0.87-0.91 of the copy;
-// what is left is the launch, the share's beginning and the second kernel (8 us together).  What it had been bound by: 920 instructions a
-// warp and tile, most of them addresses (140 us); now 16 loads of operands, 32 products, 32 requests.  On tcgen05, whose tile of 128
-// rows would be 7 / 128 full, the same 123 us, but a short call takes 2 us more, and pages that TMA cannot bring 168 us.
+// One row of 28 query over 4 key heads for four sequences of 40007 to 131072 keys (700 MB): 116 us in a captured graph, 6.0 TB/s, 0.92 of the copy,
+// and 118 to 128 a call in a stream of calls, by the board (0.84 to 0.91); what is left is the launch, the share's beginning and the second
+// kernel (8 us together).  What it had been bound by: 920 instructions a warp and tile, most of them addresses (140 us); now 16 loads of
+// operands, 32 products, 32 requests.  On tcgen05, whose tile of 128 rows would be 7 / 128 full, the same time, but a short call takes 2 us
+// more, and pages that TMA cannot bring 168 us.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

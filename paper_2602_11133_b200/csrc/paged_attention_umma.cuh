@@ -29,11 +29,14 @@
 // The softmax warps bring the queries themselves, when a part begins: their room is the one that the previous part has left through.
 //
 // 32 rows of 32 heads of 16 sequences of 384 to 704 keys (143 MB): 45 us, 3.3 TB/s; bound by the chain a short item is (queries, first
-// scores, exponentials, second product, way out: 10 us for its four tiles), which two streams hide half of.  Before: 59.5 us on
+// scores, exponentials, second product, way out: 11 to 12 us for its four tiles), which two streams hide half of.  Before: 59.5 us on
 // mma.sync in tiles of 32 rows, 66 as one stream of even and odd tiles, which ended its items together.
 // 224 rows a key head of eight sequences of 2001 to 9001 keys (20 GFLOP): 49 us, 410 TFLOP/s; bound by the exponentials' chain (1.45k cycles for
 // 64 keys of 128 rows, 0.6k of them until the stores to tensor memory are done, which share it with the other products) and by start and end
-// of a part (8k cycles); 104 us on mma.sync, 51.5 with one score buffer of 128 keys.  704 rows over 704 keys: 630 TFLOP/s.
+// of a part (8k cycles); 104 us on mma.sync, 51.5 with one score buffer of 128 keys.  Canvases of 704 rows over 704 keys, 32 heads
+// of 16 sequences: 202 us, 640 TFLOP/s.  With keys by cp.async (pages of 100 keys) the first two take 51 and 47 us.
+// Registers: 168 a thread with 384 threads, of which 128 columns with 32 and 64 rows exceed by 32 and 20 bytes of local memory; 128 with 448 threads
+// (by cp.async), by 20 to 168 bytes in all forms but 64 columns with 256 rows.
 //
 // Every barrier is waited on phase by phase by whoever waits on it, so that a parity says which phase is meant.  All waits end: one
 // that gives up makes the CTA leave, after its copies and products under way have ended.
@@ -58,7 +61,9 @@ struct UmmaPagedRoles {
     static constexpr int PROD = 8, PROD_WARPS = TMA ? 1 : (TWO ? 4 : 2);       // of a stream (TWO: of both)
     static constexpr int MMA = TMA ? 10 : 12, THREADS = TMA ? 384 : 448;
 };
-// Keys of a tile that TMA brings, and whether it can: whole pages in 128 rows, or parts of 128 of a page.
+// Keys of a tile that TMA brings, and whether it can: whole pages in 128 rows, or parts of 128 of a page.  Pages of 72 to 120 keys leave up to 44 % of a
+// tile empty; 32 rows of 32 heads are the faster for it all the same (48.5 us at 72 keys, 42.9 at 120; by cp.async 51.5), 224 rows from 120 keys on
+// (60.3 us at 72, 52.3 at 96, 46.7 at 120; by cp.async 47.4).
 __host__ __device__ constexpr bool paged_tma_pages(int page_size) { return page_size % 8 == 0 && (page_size <= 128 || page_size % 128 == 0); }
 __host__ __device__ constexpr int paged_tma_keys(int page_size) { return page_size <= 128 ? 128 / page_size * page_size : 128; }
 
