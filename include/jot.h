@@ -204,8 +204,8 @@ int jot_read_status(jot_model* m, void* stream);
  *   refresh == 0  only rows [blk_lo, blk_hi) go through the network; in every layer their fresh keys and
  *                 values replace the cache's entries for those positions and their queries attend over
  *                 all L positions, the others as cached.  Needs an earlier refresh with the same B and L
- *                 (else JOT_ERR_ARG); one that failed, or whose failure a status read since has reported,
- *                 leaves no canvas, and neither does a jot_generate with kv_cache.  Per step this costs (blk_hi - blk_lo) / L of the full pass's
+ *                 (else JOT_ERR_ARG); one that failed (without jot_set_sync's synchronisation: from the
+ *                 status read on that reports it) leaves no canvas, and neither does a jot_generate with kv_cache.  Per step this costs (blk_hi - blk_lo) / L of the full pass's
  *                 projections; its statistics are approximate wherever the canvas has changed outside
  *                 the block since the refresh.
  * The cache is caller-owned device memory of jot_kv_cache_bytes(cfg, max_batch, max_seq) bytes, 1 KiB

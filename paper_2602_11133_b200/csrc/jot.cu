@@ -496,7 +496,7 @@ struct jot_model {
     std::vector<CUtensorMap> kv_tm_qkv3, kv_tm_vt;
     int kv_map_B = -1, kv_map_L = -1;       // geometry the per-layer maps were encoded for
     int kv_valid_B = -1, kv_valid_L = -1;   // geometry of the last refresh (block passes need one)
-    bool kv_unread = false;                 // a refresh has been enqueued whose status nobody has read yet
+    bool kv_unread = false;                 // a refresh has been enqueued whose status nobody has read yet: ctrl[4] holds what it was behind it
     // the same cache in pages instead (caller's memory too): keys and values only, wherever the page table says
     bool paged = false;
     jot_kv_pages pages;
@@ -937,18 +937,19 @@ int check_step_args(const jot_model* m, const void* tokens, int B, int L, int bl
 bool status_of_input(int32_t w) { return w == kStatusBadToken || w == kStatusBadIndex; }
 int status_code(int32_t w) { return w == 0 ? JOT_OK : (status_of_input(w) ? JOT_ERR_ARG : JOT_ERR_TIMEOUT); }
 
-// A status word that has been read, as a call's result.
-int take_status(jot_model* m, int32_t w, cudaStream_t st) {
-    if (w != 0 && m->kv_unread) m->kv_valid_B = m->kv_valid_L = -1;           // it may be the refresh's: the cache holds a mixture then
+// A status word that has been read, as a call's result; `behind_refresh`: what it was behind a refresh that nobody has asked about yet (where that is
+// not at hand, the word itself).
+int take_status(jot_model* m, int32_t w, int32_t behind_refresh, cudaStream_t st) {
+    if (behind_refresh != 0 && m->kv_unread) m->kv_valid_B = m->kv_valid_L = -1;      // the cache holds a mixture
     m->kv_unread = false;
     if (status_of_input(w)) JOT_CUDA(cudaMemsetAsync(m->ctrl, 0, 4, st));     // the caller can fix its input and go on
     return status_code(w);
 }
 
 int read_status(jot_model* m, cudaStream_t st) {
-    JOT_CUDA(cudaMemcpyAsync(m->h_pinned, m->ctrl, 4, cudaMemcpyDeviceToHost, st));
+    JOT_CUDA(cudaMemcpyAsync(m->h_pinned, m->ctrl, m->kv_unread ? 20 : 4, cudaMemcpyDeviceToHost, st));
     JOT_CUDA(cudaStreamSynchronize(st));
-    return take_status(m, m->h_pinned[0], st);
+    return take_status(m, m->h_pinned[0], m->h_pinned[4], st);
 }
 
 int launch_accept(const AcceptArgs& a, cudaStream_t st, const AcceptParamsInline* inl = nullptr) {
@@ -1280,8 +1281,12 @@ int jot_denoise_step_cached(jot_model* m, const int32_t* d_tokens, int B, int L,
     const FwdSpan span = refresh ? FwdSpan{L, 0, true, true} : FwdSpan{blk_hi - blk_lo, blk_lo, true, false};
     const int rc = denoise_step_impl(m, d_tokens, B, L, blk_lo, blk_hi, exclude_mask_token, d_bump_id, d_bump_val, d_top1,
                                      d_top2, d_sumexp, d_argmax, sampling, d_sampled, stream, &span);
-    if (rc == JOT_OK && refresh) { m->kv_valid_B = B; m->kv_valid_L = L; m->kv_unread = !m->sync_steps; }
-    return rc;
+    if (rc != JOT_OK || !refresh) return rc;
+    if (!m->sync_steps) JOT_CUDA(cudaMemcpyAsync(m->ctrl + 4, m->ctrl, 4, cudaMemcpyDeviceToDevice, (cudaStream_t)stream));
+    m->kv_valid_B = B;
+    m->kv_valid_L = L;
+    m->kv_unread = !m->sync_steps;
+    return JOT_OK;
 }
 
 int jot_accept_freeze(const jot_params* params, int per_seq_params, int32_t mask_id, int32_t* d_tokens, int B, int L,
@@ -1350,7 +1355,7 @@ int jot_generate(jot_model* m, const jot_params* params, int per_seq_params, con
     auto outcome = [&](int slot, bool* finished) -> int {      // wait for a step's control words
         JOT_CUDA(cudaEventSynchronize(m->step_done[slot]));
         const int32_t* w = m->h_pinned + 4 * slot;
-        if (w[0]) return take_status(m, w[0], st);
+        if (w[0]) return take_status(m, w[0], w[0], st);
         *finished = w[2] == 0;
         if (!*finished) B_act = w[2];
         return JOT_OK;
@@ -1400,7 +1405,7 @@ int jot_generate(jot_model* m, const jot_params* params, int per_seq_params, con
                 }
                 JOT_CUDA(cudaMemcpyAsync(m->h_pinned, m->ctrl, 16, cudaMemcpyDeviceToHost, st));
                 JOT_CUDA(cudaStreamSynchronize(st));
-                if (m->h_pinned[0]) return take_status(m, m->h_pinned[0], st);
+                if (m->h_pinned[0]) return take_status(m, m->h_pinned[0], m->h_pinned[0], st);
                 ++n_passes;
                 if (m->h_pinned[2] == 0) break;              // no sequence has a masked position left in this block
             }

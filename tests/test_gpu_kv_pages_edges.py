@@ -115,6 +115,33 @@ def test_a_refresh_that_failed_leaves_no_canvas(jot, paged, sync):
     model.close()
 
 
+def test_a_later_failure_is_not_the_refresh_s(jot):
+    """Without a read in between, the refresh's own outcome tells whether there is a canvas, not what a later step met."""
+    g, model, canvas, lo, hi = small(jot)
+    _, table = in_pages(jot, model, g, 2, canvas.shape[1], 16)
+    block = lambda c=canvas: model.denoise_step_cached(c, lo, hi, refresh=False)
+    model.denoise_step_cached(canvas, lo, hi, refresh=True)
+    want = block().sumexp.clone()
+    bad = canvas.clone()
+    bad[0, lo] = g.vocab + 3
+    model.set_sync(False)
+    for later in (lambda: block(bad), lambda: model.denoise_step(bad, lo, hi)):
+        model.denoise_step_cached(canvas, lo, hi, refresh=True)
+        later()
+        refused(jot, -1, model.read_status)
+        assert torch.equal(block().sumexp, want)
+        model.read_status()
+    # and the other way about: the steps behind a refresh that failed change nothing about it
+    good = table.clone()
+    table[1, 1] = 10 ** 6
+    model.denoise_step_cached(canvas, lo, hi, refresh=True)
+    table.copy_(good)
+    block()
+    refused(jot, -1, model.read_status)
+    refused(jot, -1, block)
+    model.close()
+
+
 def test_a_generation_that_failed_leaves_no_canvas(jot):
     g, model, canvas, lo, hi = small(jot)
     _, table = in_pages(jot, model, g, 2, canvas.shape[1], 16)
